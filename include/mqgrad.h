@@ -393,6 +393,108 @@ void mqg_adaptive_default_config(mqg_adaptive_config* cfg);
 mqg_status mqg_adaptive_bits(const double* worker_norms, uint32_t W, const mqg_adaptive_config* cfg,
                              uint32_t* bits_out);
 
+/* ---- before the exchange: gradients of any type, their common norm, and clipping ----------------------
+ *
+ * A large model's gradients come in half precision, in hundreds of tensors, and are scaled down to a given norm before
+ * they are exchanged; the quantizer above takes finite fp32 values.  These calls take tensors of any of the three types
+ * as they are, all of them in a few launches:
+ *
+ *   norm = sqrt(sum over all tensors and values of x^2)     squares and sums in fp64
+ *   c    = 1 where norm <= max_norm, else (float)(max_norm / norm);  a norm that is not a number makes c one too
+ *   y    = x * c, one fp32 product, rounded once to the output's type
+ *
+ * Where a gradient is quantized already, its scales (or ranges) are clipped in its stead: a bucket's levels are
+ * proportional to its scale, so mqg_global_norm of the gradients and mqg_clip_by_norm of the scales give the clipped
+ * gradient's stream at n / bucket values' cost. */
+
+typedef enum { MQG_FLOAT32 = 0, MQG_FLOAT16 = 1, MQG_BFLOAT16 = 2 } mqg_dtype;
+
+#define MQG_MAX_NORM_TENSORS 65536u
+
+typedef struct {
+    const void* data;     /* device, n values of dtype, aligned to one value */
+    void* out;            /* device, n values of out_dtype; may be `data` itself where the types are equal.  Not read by mqg_global_norm. */
+    uint64_t n;           /* 0 is allowed (the tensor is skipped) */
+    mqg_dtype dtype;
+    mqg_dtype out_dtype;  /* not read by mqg_global_norm */
+} mqg_clip_item;
+
+/* The norm of all `count` tensors together; reproducible to the bit (the order of all additions depends on the sizes
+ * only).  A tensor named twice counts twice.
+ *   items       HOST array of `count` tensors, at most MQG_MAX_NORM_TENSORS, read during the call only.
+ *   workspace   device, mqg_global_norm_workspace_bytes(count) bytes of scratch memory, 8-byte aligned; contents on
+ *               entry are of no interest, contents on return are unspecified.  Calls that share a workspace must not overlap.
+ *   norm_out    device, one double, 8-byte aligned, overwritten (0 where there are no values).
+ * Errors: MQG_EINVAL (NULL pointer, unknown type, too many tensors or over 10^13 values), MQG_EALIGN, MQG_ELAUNCH. */
+size_t mqg_global_norm_workspace_bytes(uint32_t count);
+mqg_status mqg_global_norm(const mqg_clip_item* items, uint32_t count, void* workspace, double* norm_out, void* stream);
+
+/* y for all `count` tensors, with a norm that is on the device already: one that mqg_global_norm left there, or one that was
+ * combined from several shards'.
+ *   norm      device, one double, 8-byte aligned; must not lie in an output.
+ *   max_norm  not negative; infinity clips nothing.
+ * Errors as for mqg_global_norm; MQG_EINVAL also where max_norm is negative or not a number, and where an output lies over
+ * any other tensor's values or output, or over its own tensor's without being that tensor.  MQG_ELAUNCH also where the host
+ * has no memory for that check. */
+mqg_status mqg_clip_by_norm(const mqg_clip_item* items, uint32_t count, const double* norm, double max_norm, void* stream);
+
+/* mqg_global_norm, then mqg_clip_by_norm with that norm.  Arguments and errors as above; neither workspace nor norm_out may
+ * lie in an output. */
+mqg_status mqg_clip_global_norm(const mqg_clip_item* items, uint32_t count, double max_norm, void* workspace, double* norm_out,
+                                void* stream);
+
+/* ---- rows by token: the parameters that a worker pulls, and their gradient ----------------------------
+ *
+ * A language model's largest tensor is its table of embeddings, of which a batch uses the rows of its tokens.  The
+ * server's (or a shard's) rows are looked up by token, and the gradient of the rows is added up by token, either as a
+ * whole table (which is clipped, quantized and exchanged like any other layer) or straight into the parameters:
+ *
+ *   lookup    out[p, :]   = scale * table[id_p - first_row, :]          (fp32 product, rounded once to out's type)
+ *   gradient  grad[r, :]  = scale * S_r,                                S_r = sum over the positions p with
+ *             grad[r, :] += scale * S_r  (accumulate)                   id_p - first_row = r of grad_out[p, :]
+ *
+ * A token outside [first_row, first_row + rows) belongs to another shard (or is a filler such as -1): its row of `out` is
+ * zero and its position adds to no row.  S_r is summed in fp32 in an order that depends on the tokens only (equal inputs
+ * give equal bits) and rounded once, after the product with scale and the addition to the old value.  Every row that no
+ * token names becomes zero; with `accumulate` it is left untouched.  With scale = -lr (or -lr / W for the positions of W
+ * workers, one after the other), accumulate and the parameters in the place of grad, that is the server's SGD step from
+ * gradients that are sparse by rows. */
+
+typedef enum { MQG_INDEX32 = 0, MQG_INDEX64 = 1 } mqg_index_type;
+
+#define MQG_MAX_TOKENS 0x7FFFFFFFu
+#define MQG_MAX_TABLE_ROWS 0x7FFFFFFFu
+#define MQG_MAX_ROW_DIM 0x1000000u
+
+typedef struct {
+    void* data;       /* device, aligned to one value; values [r * stride, r * stride + dim) are row r.  Written only where the call says so. */
+    uint64_t rows;
+    uint64_t stride;  /* a matrix that is written: at least dim (or one row); one that is read: any, 0 repeats one row */
+    mqg_dtype dtype;
+} mqg_rows;
+
+typedef struct {
+    const void* ids;      /* device, `count` signed integers, aligned to one */
+    uint64_t count;       /* 0 is allowed */
+    mqg_index_type type;
+    int64_t first_row;    /* token of the table's first row, 0 .. 2^62 */
+    int64_t padding_id;   /* gradient only: positions of this token add to no row; a token that cannot occur (INT64_MIN) for none */
+} mqg_tokens;
+
+/* table: `rows` rows, read; out: tokens->count rows, overwritten (data may be NULL where there are none).  1 <= dim <= MQG_MAX_ROW_DIM.
+ * Errors: MQG_EINVAL (NULL pointer, size or type out of range, rows of `out` that overlap each other, out->rows other than
+ * tokens->count, `out` over the table or the tokens), MQG_EALIGN, MQG_ELAUNCH. */
+mqg_status mqg_embedding(const mqg_rows* table, const mqg_tokens* tokens, uint32_t dim, float scale, const mqg_rows* out, void* stream);
+
+/* grad_out: tokens->count rows, read; table_grad: `rows` rows, overwritten or added to.
+ *   workspace   device, mqg_embedding_grad_workspace_bytes(tokens->count, dim, table_grad->rows) bytes of scratch memory, 16-byte
+ *               aligned; contents on entry are of no interest, contents on return are unspecified.  Calls that share a
+ *               workspace must not overlap.  May be NULL where that size is 0.
+ * Errors as for mqg_embedding. */
+size_t mqg_embedding_grad_workspace_bytes(uint64_t tokens, uint32_t dim, uint64_t rows);
+mqg_status mqg_embedding_grad(const mqg_rows* grad_out, const mqg_tokens* tokens, uint32_t dim, float scale, const mqg_rows* table_grad,
+                              int accumulate, void* workspace, void* stream);
+
 /* ---- host-side agent that chooses K (Section 3.3, Algorithm 2).  No GPU involved. ---------- */
 
 typedef struct mqg_mdp mqg_mdp;

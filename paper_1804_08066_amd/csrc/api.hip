@@ -1,5 +1,9 @@
 // C-ABI layer of libmqgrad: argument validation and launch set-up.  No arithmetic of the method
-// happens here; the kernels are in quantize_pack.hip, quantize_wave.hip, aggregate_update.hip and minmax.hip.
+// happens here; the kernels are in quantize_pack.hip, quantize_wave.hip, aggregate_update.hip, minmax.hip, requantize_cells.hip,
+// grad_norm.hip and embedding.hip.
+
+#include <algorithm>
+#include <new>
 
 #include "kernels.h"
 
@@ -146,6 +150,119 @@ mqg_status update_batch_args(const mqg_update_item* items, uint32_t count, uint3
     a.pointers = used;
     *tiles_out = (uint32_t)tiles;
     return MQG_OK;
+}
+
+uint32_t size_of(mqg_dtype t) { return t == MQG_FLOAT32 ? 4u : (t == MQG_FLOAT16 || t == MQG_BFLOAT16 ? 2u : 0u); }   // 0: no such type
+bool misaligned(const void* p, uint32_t size) { return (reinterpret_cast<uintptr_t>(p) & (size - 1u)) != 0; }
+
+// a range of memory; `item`: whose
+struct Span {
+    uintptr_t at, end;
+    uint32_t item;
+    bool written;
+};
+bool overlap(const Span& a, const Span& b) { return a.at < b.end && b.at < a.end; }
+
+// Whether a written span of `spans` lies over any other, an item's own two being the same span excepted.  Sorts them.
+bool writes_collide(Span* spans, uint32_t count) {
+    std::sort(spans, spans + count, [](const Span& a, const Span& b) { return a.at < b.at; });
+    // the span seen so far that ends last, and the last such of another item; of the written ones, and of all
+    struct Last {
+        Span first = {0, 0, 0, false}, other = {0, 0, 0, false};
+        void add(const Span& s) {
+            if (s.item == first.item) {
+                if (s.end > first.end) first = s;
+            } else if (s.end > first.end) {
+                other = first;
+                first = s;
+            } else if (s.end > other.end) {
+                other = s;
+            }
+        }
+        bool over(const Span& s) const { return (first.item != s.item ? first : other).end > s.at; }
+    } written, all;
+    for (uint32_t i = 0; i < count; ++i) {
+        if (written.over(spans[i]) || (spans[i].written && all.over(spans[i]))) return true;
+        all.add(spans[i]);
+        if (spans[i].written) written.add(spans[i]);
+    }
+    return false;
+}
+
+mqg_status norm_items(const mqg_clip_item* items, uint32_t count) {
+    if (count > MQG_MAX_NORM_TENSORS || (count > 0u && items == nullptr)) return MQG_EINVAL;
+    uint64_t values = 0;
+    for (uint32_t i = 0; i < count; ++i) {
+        const mqg_clip_item& it = items[i];
+        if (size_of(it.dtype) == 0u) return MQG_EINVAL;
+        if (it.n == 0) continue;
+        if (it.data == nullptr || it.n > mqg::norm_max_values() - values) return MQG_EINVAL;
+        values += it.n;
+        if (misaligned(it.data, size_of(it.dtype))) return MQG_EALIGN;
+    }
+    return MQG_OK;
+}
+// the outputs of a clipping call; norm_items first.  scratch, scratch_bytes: what the call writes besides
+mqg_status clip_items(const mqg_clip_item* items, uint32_t count, double max_norm, const void* norm, const void* scratch, size_t scratch_bytes) {
+    if (!(max_norm >= 0.0)) return MQG_EINVAL;
+    for (uint32_t i = 0; i < count; ++i) {
+        const mqg_clip_item& it = items[i];
+        if (size_of(it.out_dtype) == 0u) return MQG_EINVAL;
+        if (it.n == 0) continue;
+        if (it.out == nullptr) return MQG_EINVAL;
+        if (misaligned(it.out, size_of(it.out_dtype))) return MQG_EALIGN;
+    }
+    constexpr uint32_t kFew = 64;
+    Span few[2u * kFew + 2u];
+    Span* spans = count <= kFew ? few : new (std::nothrow) Span[2u * count + 2u];
+    if (spans == nullptr) return MQG_ELAUNCH;
+    uint32_t used = 0;
+    bool bad = false;
+    const auto span = [](const void* p, uint64_t bytes, uint32_t item, bool written) {
+        const uintptr_t at = reinterpret_cast<uintptr_t>(p);
+        return Span{at, at + bytes, item, written};
+    };
+    for (uint32_t i = 0; i < count; ++i) {
+        const mqg_clip_item& it = items[i];
+        if (it.n == 0) continue;
+        const Span in = span(it.data, it.n * size_of(it.dtype), i + 1u, false), out = span(it.out, it.n * size_of(it.out_dtype), i + 1u, true);
+        const bool in_place = it.data == it.out && it.dtype == it.out_dtype;
+        bad = bad || (!in_place && overlap(in, out));
+        if (!in_place) spans[used++] = in;
+        spans[used++] = out;
+    }
+    spans[used++] = span(norm, sizeof(double), count + 1u, false);
+    if (scratch_bytes != 0) spans[used++] = span(scratch, scratch_bytes, count + 2u, false);
+    bad = bad || writes_collide(spans, used);
+    if (spans != few) delete[] spans;
+    return bad ? MQG_EINVAL : MQG_OK;
+}
+
+// a matrix's memory, from its first value to behind its last
+Span span_of(const mqg_rows& m, uint32_t dim) {
+    const uintptr_t at = reinterpret_cast<uintptr_t>(m.data);
+    return {at, m.rows == 0 ? at : at + ((m.rows - 1u) * m.stride + dim) * size_of(m.dtype), 0, false};
+}
+mqg_status rows_args(const mqg_rows* m, uint64_t most_rows, uint32_t dim, bool written, mqg::RowMatrix& out) {
+    if (m == nullptr || size_of(m->dtype) == 0u || m->rows > most_rows) return MQG_EINVAL;
+    if (m->rows > 1u && m->stride > (UINT64_MAX >> 4) / m->rows) return MQG_EINVAL;
+    if (written && m->rows > 1u && m->stride < dim) return MQG_EINVAL;
+    if (m->rows > 0u && m->data == nullptr) return MQG_EINVAL;
+    if (misaligned(m->data, size_of(m->dtype))) return MQG_EALIGN;
+    out = mqg::RowMatrix{m->data, m->rows, m->stride, (int)m->dtype};
+    return MQG_OK;
+}
+mqg_status tokens_args(const mqg_tokens* t, mqg::TokenIds& out) {
+    if (t == nullptr || (t->type != MQG_INDEX32 && t->type != MQG_INDEX64) || t->count > MQG_MAX_TOKENS) return MQG_EINVAL;
+    if (t->first_row < 0 || t->first_row > ((int64_t)1 << 62)) return MQG_EINVAL;
+    if (t->count > 0u && t->ids == nullptr) return MQG_EINVAL;
+    if (misaligned(t->ids, t->type == MQG_INDEX64 ? 8u : 4u)) return MQG_EALIGN;
+    out = mqg::TokenIds{t->ids, t->count, t->type == MQG_INDEX64 ? 1 : 0, t->first_row, t->padding_id};
+    return MQG_OK;
+}
+Span span_of(const mqg_tokens& t) {
+    const uintptr_t at = reinterpret_cast<uintptr_t>(t.ids);
+    return {at, at + t.count * (t.type == MQG_INDEX64 ? 8u : 4u), 0, false};
 }
 
 }  // namespace
@@ -623,6 +740,80 @@ mqg_status mqg_sum_squares_batch_static(const mqg_sumsq_item* items, uint32_t co
     const mqg_status st = sumsq_batch_args(items, count, sumsq_out, b);   // count > MQG_MAX_SUMSQ_TENSORS: MQG_EINVAL
     if (st != MQG_OK) return st;
     const hipError_t err = mqg::launch_sum_squares_batch_static(b, count, sumsq_out, static_cast<hipStream_t>(stream));
+    return err == hipSuccess ? MQG_OK : MQG_ELAUNCH;
+}
+
+size_t mqg_global_norm_workspace_bytes(uint32_t count) { return sizeof(double) * (size_t)mqg::norm_partials(count); }
+
+mqg_status mqg_global_norm(const mqg_clip_item* items, uint32_t count, void* workspace, double* norm_out, void* stream) {
+    const mqg_status st = norm_items(items, count);
+    if (st != MQG_OK) return st;
+    if (norm_out == nullptr || (count > 0u && workspace == nullptr)) return MQG_EINVAL;
+    if (misaligned8(norm_out) || misaligned8(workspace)) return MQG_EALIGN;
+    const hipError_t err = mqg::launch_global_norm(items, count, static_cast<double*>(workspace), norm_out, static_cast<hipStream_t>(stream));
+    return err == hipSuccess ? MQG_OK : MQG_ELAUNCH;
+}
+
+mqg_status mqg_clip_by_norm(const mqg_clip_item* items, uint32_t count, const double* norm, double max_norm, void* stream) {
+    mqg_status st = norm_items(items, count);
+    if (st != MQG_OK) return st;
+    if (norm == nullptr) return MQG_EINVAL;
+    if (misaligned8(norm)) return MQG_EALIGN;
+    st = clip_items(items, count, max_norm, norm, nullptr, 0);
+    if (st != MQG_OK) return st;
+    const hipError_t err = mqg::launch_clip(items, count, norm, max_norm, static_cast<hipStream_t>(stream));
+    return err == hipSuccess ? MQG_OK : MQG_ELAUNCH;
+}
+
+mqg_status mqg_clip_global_norm(const mqg_clip_item* items, uint32_t count, double max_norm, void* workspace, double* norm_out,
+                                void* stream) {
+    mqg_status st = norm_items(items, count);
+    if (st != MQG_OK) return st;
+    if (norm_out == nullptr || (count > 0u && workspace == nullptr)) return MQG_EINVAL;
+    if (misaligned8(norm_out) || misaligned8(workspace)) return MQG_EALIGN;
+    st = clip_items(items, count, max_norm, norm_out, workspace, mqg_global_norm_workspace_bytes(count));
+    if (st != MQG_OK) return st;
+    hipError_t err = mqg::launch_global_norm(items, count, static_cast<double*>(workspace), norm_out, static_cast<hipStream_t>(stream));
+    if (err == hipSuccess) err = mqg::launch_clip(items, count, norm_out, max_norm, static_cast<hipStream_t>(stream));
+    return err == hipSuccess ? MQG_OK : MQG_ELAUNCH;
+}
+
+mqg_status mqg_embedding(const mqg_rows* table, const mqg_tokens* tokens, uint32_t dim, float scale, const mqg_rows* out, void* stream) {
+    if (dim < 1u || dim > MQG_MAX_ROW_DIM) return MQG_EINVAL;
+    mqg::RowMatrix t, o;
+    mqg::TokenIds ids;
+    mqg_status st = rows_args(table, MQG_MAX_TABLE_ROWS, dim, false, t);
+    if (st == MQG_OK) st = tokens_args(tokens, ids);
+    if (st == MQG_OK) st = rows_args(out, MQG_MAX_TOKENS, dim, true, o);
+    if (st != MQG_OK) return st;
+    if (table->rows == 0u || out->rows != tokens->count) return MQG_EINVAL;
+    if (overlap(span_of(*out, dim), span_of(*table, dim)) || overlap(span_of(*out, dim), span_of(*tokens))) return MQG_EINVAL;
+    const hipError_t err = mqg::launch_embedding(t, ids, dim, scale, o, static_cast<hipStream_t>(stream));
+    return err == hipSuccess ? MQG_OK : MQG_ELAUNCH;
+}
+
+size_t mqg_embedding_grad_workspace_bytes(uint64_t tokens, uint32_t dim, uint64_t rows) {
+    if (tokens > MQG_MAX_TOKENS || rows < 1u || rows > MQG_MAX_TABLE_ROWS || dim < 1u || dim > MQG_MAX_ROW_DIM) return 0;   // which the call refuses
+    return mqg::embedding_grad_workspace(tokens, dim, rows);
+}
+
+mqg_status mqg_embedding_grad(const mqg_rows* grad_out, const mqg_tokens* tokens, uint32_t dim, float scale, const mqg_rows* table_grad,
+                              int accumulate, void* workspace, void* stream) {
+    if (dim < 1u || dim > MQG_MAX_ROW_DIM) return MQG_EINVAL;
+    mqg::RowMatrix g, o;
+    mqg::TokenIds ids;
+    mqg_status st = rows_args(grad_out, MQG_MAX_TOKENS, dim, false, g);
+    if (st == MQG_OK) st = tokens_args(tokens, ids);
+    if (st == MQG_OK) st = rows_args(table_grad, MQG_MAX_TABLE_ROWS, dim, true, o);
+    if (st != MQG_OK) return st;
+    if (table_grad->rows == 0u || grad_out->rows != tokens->count) return MQG_EINVAL;
+    const size_t need = mqg::embedding_grad_workspace(ids.count, dim, o.rows);
+    if (need != 0 && workspace == nullptr) return MQG_EINVAL;
+    if (misaligned(workspace, 16u)) return MQG_EALIGN;
+    const uintptr_t ws = reinterpret_cast<uintptr_t>(workspace);
+    const Span out = span_of(*table_grad, dim), in = span_of(*grad_out, dim), at = span_of(*tokens), scratch = {ws, ws + need, 0, false};
+    if (overlap(out, in) || overlap(out, at) || overlap(out, scratch) || overlap(in, scratch) || overlap(at, scratch)) return MQG_EINVAL;
+    const hipError_t err = mqg::launch_embedding_grad(g, ids, dim, scale, o, accumulate != 0, workspace, static_cast<hipStream_t>(stream));
     return err == hipSuccess ? MQG_OK : MQG_ELAUNCH;
 }
 

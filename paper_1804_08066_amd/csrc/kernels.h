@@ -232,4 +232,43 @@ hipError_t launch_sum_squares_batch(const SumSquaresBatch& b, uint32_t count, do
 // the same with the partial sums in a device array the library holds (no allocation, no workspace argument)
 hipError_t launch_sum_squares_batch_static(const SumSquaresBatch& b, uint32_t count, double* out, hipStream_t stream);
 
+// grad_norm.hip: tensors of one launch, of any of the three types.  A list longer than a table takes several launches.
+template <uint32_t TENSORS>
+struct TensorTable {
+    static constexpr uint32_t kTensors = TENSORS;
+    uint32_t count, pieces;
+    uint32_t start[TENSORS];   // prefix sums of the tensors' pieces
+    const void* data[TENSORS];
+    uint64_t n[TENSORS];
+    uint8_t dtype[TENSORS];
+};
+using NormTable = TensorTable<192>;
+struct ClipTable : TensorTable<128> {
+    void* out[128];
+    uint8_t out_dtype[128];
+};
+constexpr uint32_t kNormBlocks = 2048;   // workgroups of a launch, and partial sums that it stores
+inline uint32_t norm_partials(uint32_t count) { return (count + NormTable::kTensors - 1u) / NormTable::kTensors * kNormBlocks; }
+uint64_t norm_max_values();              // of all tensors together
+// `items` are checked; items without values are skipped
+hipError_t launch_global_norm(const mqg_clip_item* items, uint32_t count, double* partials, double* norm, hipStream_t stream);
+hipError_t launch_clip(const mqg_clip_item* items, uint32_t count, const double* norm, double max_norm, hipStream_t stream);
+
+// embedding.hip
+struct RowMatrix {
+    void* data;
+    uint64_t rows, stride;   // stride: values from one row to the next
+    int dtype;
+};
+struct TokenIds {
+    const void* ids;
+    uint64_t count;
+    int wide;                // 1: 64-bit ids
+    int64_t first_row, padding;
+};
+hipError_t launch_embedding(const RowMatrix& table, const TokenIds& ids, uint32_t dim, float scale, const RowMatrix& out, hipStream_t stream);
+size_t embedding_grad_workspace(uint64_t tokens, uint32_t dim, uint64_t rows);
+hipError_t launch_embedding_grad(const RowMatrix& grad_out, const TokenIds& ids, uint32_t dim, float scale, const RowMatrix& table_grad,
+                                 bool accumulate, void* workspace, hipStream_t stream);
+
 }  // namespace mqg

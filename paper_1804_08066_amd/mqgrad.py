@@ -15,6 +15,8 @@ MQG_OK, MQG_EINVAL, MQG_EALIGN, MQG_ELAUNCH = 0, -1, -2, -3
 MQG_SCALE_MAXABS, MQG_SCALE_L2 = 0, 1
 MQG_CODES_MAY_BE_CACHED, MQG_CODES_FROM_MEMORY = 0, 1
 MQG_CODES_KEEP_CACHED, MQG_CODES_TO_MEMORY = 0, 1
+MQG_FLOAT32, MQG_FLOAT16, MQG_BFLOAT16 = 0, 1, 2
+MQG_INDEX32, MQG_INDEX64 = 0, 1
 MQG_MAX_WORKERS = 64
 
 EXPORTS = [
@@ -30,6 +32,8 @@ EXPORTS = [
     "mqg_sum_squares_workspace_bytes", "mqg_sum_squares_batch", "mqg_sum_squares_batch_static",
     "mqg_quantize_minmax_tensors", "mqg_aggregate_update_minmax_tensors", "mqg_aggregate_requantize_mode",
     "mqg_aggregate_update_from", "mqg_quantize_to",
+    "mqg_global_norm_workspace_bytes", "mqg_global_norm", "mqg_clip_by_norm", "mqg_clip_global_norm",
+    "mqg_embedding", "mqg_embedding_grad_workspace_bytes", "mqg_embedding_grad",
 ]
 
 
@@ -63,6 +67,18 @@ class QuantizeItem(C.Structure):
 class UpdateItem(C.Structure):
     _fields_ = [("n", C.c_uint64), ("params", C.c_void_p), ("packed", C.POINTER(C.c_void_p)),
                 ("scales", C.POINTER(C.c_void_p)), ("raw", C.POINTER(C.c_void_p))]
+
+
+class ClipItem(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("out", C.c_void_p), ("n", C.c_uint64), ("dtype", C.c_int), ("out_dtype", C.c_int)]
+
+
+class Rows(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("rows", C.c_uint64), ("stride", C.c_uint64), ("dtype", C.c_int)]
+
+
+class Tokens(C.Structure):
+    _fields_ = [("ids", C.c_void_p), ("count", C.c_uint64), ("type", C.c_int), ("first_row", C.c_int64), ("padding_id", C.c_int64)]
 
 
 MQG_MAX_TENSORS = 32
@@ -146,6 +162,20 @@ def lib():
     L.mqg_sum_squares_batch.restype = C.c_int
     L.mqg_sum_squares_batch_static.argtypes = [C.POINTER(SumsqItem), u32, vp, vp]
     L.mqg_sum_squares_batch_static.restype = C.c_int
+    L.mqg_global_norm_workspace_bytes.argtypes = [u32]
+    L.mqg_global_norm_workspace_bytes.restype = C.c_size_t
+    L.mqg_global_norm.argtypes = [C.POINTER(ClipItem), u32, vp, vp, vp]
+    L.mqg_global_norm.restype = C.c_int
+    L.mqg_clip_by_norm.argtypes = [C.POINTER(ClipItem), u32, vp, C.c_double, vp]
+    L.mqg_clip_by_norm.restype = C.c_int
+    L.mqg_clip_global_norm.argtypes = [C.POINTER(ClipItem), u32, C.c_double, vp, vp, vp]
+    L.mqg_clip_global_norm.restype = C.c_int
+    L.mqg_embedding.argtypes = [C.POINTER(Rows), C.POINTER(Tokens), u32, f32, C.POINTER(Rows), vp]
+    L.mqg_embedding.restype = C.c_int
+    L.mqg_embedding_grad_workspace_bytes.argtypes = [u64, u32, u64]
+    L.mqg_embedding_grad_workspace_bytes.restype = C.c_size_t
+    L.mqg_embedding_grad.argtypes = [C.POINTER(Rows), C.POINTER(Tokens), u32, f32, C.POINTER(Rows), C.c_int, vp, vp]
+    L.mqg_embedding_grad.restype = C.c_int
     L.mqg_adaptive_default_config.argtypes = [C.POINTER(AdaptiveConfig)]
     L.mqg_adaptive_default_config.restype = None
     L.mqg_adaptive_bits.argtypes = [C.POINTER(C.c_double), u32, C.POINTER(AdaptiveConfig), C.POINTER(u32)]
@@ -751,6 +781,185 @@ def mqg_sum_squares_batch_static(grads, out, stream=None):
     st = lib().mqg_sum_squares_batch_static(items, count, out.data_ptr(), _stream_handle(stream))
     if st != MQG_OK:
         raise MqgError(st, "mqg_sum_squares_batch_static")
+    return out
+
+
+_DTYPES = {torch.float32: MQG_FLOAT32, torch.float16: MQG_FLOAT16, torch.bfloat16: MQG_BFLOAT16}
+_INDEX_TYPES = {torch.int32: MQG_INDEX32, torch.int64: MQG_INDEX64}
+
+
+def _values(t, what):
+    """The type of a contiguous CUDA tensor of one of the three floating types, checked."""
+    if not (isinstance(t, torch.Tensor) and t.is_cuda and t.dtype in _DTYPES and t.is_contiguous()):
+        raise TypeError("%s must be a contiguous CUDA tensor of torch.float32, torch.float16 or torch.bfloat16" % what)
+    return _DTYPES[t.dtype]
+
+
+def _one_device(tensors):
+    """These calls run on the current device, where all their tensors have to be."""
+    device = torch.cuda.current_device()
+    for t in tensors:
+        if t is not None and t.get_device() != device:
+            raise ValueError("all tensors must be on the current device, cuda:%d" % device)
+
+
+def _scratch(workspace, need, stream, device, what="workspace"):
+    """A caller's workspace, checked, or one of this call's own, which the stream keeps until its work is done."""
+    if workspace is None:
+        workspace = torch.empty(need, dtype=torch.uint8, device=device)
+        if stream is not None:
+            workspace.record_stream(stream)
+        return workspace
+    if not (isinstance(workspace, torch.Tensor) and workspace.is_cuda and workspace.is_contiguous()):
+        raise TypeError("%s must be a contiguous CUDA tensor" % what)
+    if workspace.numel() * workspace.element_size() < need:
+        raise ValueError("%s must hold %d bytes" % (what, need))
+    return workspace
+
+
+def _clip_items(tensors, outputs):
+    items = (ClipItem * max(1, len(tensors)))()
+    for k, t in enumerate(tensors):
+        dtype = _values(t, "tensors[%d]" % k)
+        if outputs is None:
+            items[k] = ClipItem(t.data_ptr(), None, t.numel(), dtype, dtype)
+            continue
+        o = outputs[k]
+        out_dtype = _values(o, "outputs[%d]" % k)
+        if o.numel() != t.numel():
+            raise ValueError("outputs[%d] differs in size from its tensor" % k)
+        items[k] = ClipItem(t.data_ptr(), o.data_ptr(), t.numel(), dtype, out_dtype)
+    return items
+
+
+def mqg_global_norm_workspace_bytes(count):
+    return int(lib().mqg_global_norm_workspace_bytes(int(count)))
+
+
+def mqg_global_norm(tensors, workspace=None, norm_out=None, stream=None):
+    """The L2 norm of all the tensors together (float32, float16 and bfloat16, in any mix), reproducible to the bit, into a
+    one-element float64 device tensor.  `workspace`: a device tensor of at least mqg_global_norm_workspace_bytes(len(tensors))
+    bytes (allocated here when not given)."""
+    L, count = lib(), len(tensors)
+    items = _clip_items(tensors, None)
+    return _norm_call(L.mqg_global_norm, "mqg_global_norm", tensors, [], items, (count,), workspace, norm_out, stream)
+
+
+def _norm_call(entry, name, tensors, outputs, items, args, workspace, norm_out, stream):
+    dev = tensors[0].device if len(tensors) else "cuda"
+    if norm_out is None:
+        norm_out = torch.empty(1, dtype=torch.float64, device=dev)
+    _check(norm_out, torch.float64, "norm_out")
+    if norm_out.numel() < 1:
+        raise ValueError("norm_out must hold one value")
+    workspace = _scratch(workspace, mqg_global_norm_workspace_bytes(len(tensors)), stream, dev)
+    _one_device([*tensors, *outputs, workspace, norm_out])
+    st = entry(items, *args, workspace.data_ptr(), norm_out.data_ptr(), _stream_handle(stream))
+    if st != MQG_OK:
+        raise MqgError(st, name)
+    return norm_out
+
+
+def _outputs(tensors, outputs):
+    if outputs is None:
+        return tensors
+    if len(outputs) != len(tensors):
+        raise ValueError("outputs must have one entry per tensor")
+    return outputs
+
+
+def mqg_clip_by_norm(tensors, norm, max_norm, outputs=None, stream=None):
+    """Every tensor times min(1, max_norm / norm), for a norm that is on the device already (one float64 value); into `outputs`,
+    of any of the three types, or in place.  Returns the list of outputs."""
+    outputs = _outputs(tensors, outputs)
+    L, items = lib(), _clip_items(tensors, outputs)
+    _check(norm, torch.float64, "norm")
+    if norm.numel() < 1:
+        raise ValueError("norm must hold one value")
+    _one_device([*tensors, *outputs, norm])
+    st = L.mqg_clip_by_norm(items, len(tensors), norm.data_ptr(), max_norm, _stream_handle(stream))
+    if st != MQG_OK:
+        raise MqgError(st, "mqg_clip_by_norm")
+    return outputs
+
+
+def mqg_clip_global_norm(tensors, max_norm, outputs=None, workspace=None, norm_out=None, stream=None):
+    """mqg_global_norm of all the tensors, and every tensor scaled by min(1, max_norm / norm) into `outputs`, of any of the three
+    types, or in place.  Returns (outputs, norm)."""
+    outputs = _outputs(tensors, outputs)
+    L, items = lib(), _clip_items(tensors, outputs)
+    return outputs, _norm_call(L.mqg_clip_global_norm, "mqg_clip_global_norm", tensors, outputs, items, (len(tensors), max_norm), workspace,
+                               norm_out, stream)
+
+
+def _rows(t, what):
+    """A tensor of rows, one behind the other at one stride, and of any leading dimensions."""
+    if not (isinstance(t, torch.Tensor) and t.is_cuda and t.dtype in _DTYPES and t.dim() >= 1):
+        raise TypeError("%s must be a CUDA tensor of rows of torch.float32, torch.float16 or torch.bfloat16" % what)
+    if t.dim() != 2:
+        try:
+            t = t.view(-1, t.shape[-1]) if t.shape[-1] else t.reshape(0, 0)
+        except RuntimeError:
+            raise TypeError("%s: the leading dimensions must be one behind the other" % what) from None
+    if t.shape[1] > 1 and t.stride(1) != 1:
+        raise TypeError("%s: the values of a row must be one behind the other" % what)
+    return Rows(t.data_ptr(), t.shape[0], t.stride(0), _DTYPES[t.dtype]), t.shape[1]
+
+
+def _tokens(ids, first_row, padding_id):
+    if not (isinstance(ids, torch.Tensor) and ids.is_cuda and ids.dtype in _INDEX_TYPES and ids.is_contiguous()):
+        raise TypeError("ids must be a contiguous CUDA tensor of torch.int32 or torch.int64")
+    if not (0 <= first_row <= 1 << 62 and -(1 << 63) <= padding_id < 1 << 63):
+        raise ValueError("first_row or padding_id out of range")
+    return Tokens(ids.data_ptr(), ids.numel(), _INDEX_TYPES[ids.dtype], first_row, padding_id)
+
+
+_NO_PADDING = -(1 << 63)
+
+
+def mqg_embedding(table, ids, scale=1.0, first_row=0, out=None, stream=None):
+    """scale * table[ids - first_row], rows of zeros for tokens outside the table.  table: [rows, dim], rows at any stride; ids: int32 or
+    int64, of any shape; out: [*ids.shape, dim] of any of the three types (allocated here, in the table's type, when not given)."""
+    t, dim = _rows(table, "table")
+    tokens = _tokens(ids, first_row, _NO_PADDING)
+    if out is None:
+        out = torch.empty(*ids.shape, dim, dtype=table.dtype, device=table.device)
+    o, out_dim = _rows(out, "out")
+    if out_dim != dim or o.rows != tokens.count:
+        raise ValueError("out must hold one row of the table for every token")
+    _one_device([table, ids, out])
+    st = lib().mqg_embedding(C.byref(t), C.byref(tokens), dim, scale, C.byref(o), _stream_handle(stream))
+    if st != MQG_OK:
+        raise MqgError(st, "mqg_embedding")
+    return out
+
+
+def mqg_embedding_grad_workspace_bytes(tokens, dim, rows):
+    return int(lib().mqg_embedding_grad_workspace_bytes(tokens, dim, rows))
+
+
+def mqg_embedding_grad(grad_out, ids, rows, scale=1.0, first_row=0, padding_id=None, out=None, accumulate=False, workspace=None, stream=None):
+    """The gradient of mqg_embedding with respect to its table of `rows` rows: scale * the sum over the positions of every row's token of
+    grad_out's rows, summed in fp32 and reproducible to the bit.  Positions of padding_id add to no row.  out: [rows, dim] of any of the
+    three types, overwritten, or with accumulate=True added to (allocated here, in grad_out's type, when not given).  `workspace`: a
+    device tensor of at least mqg_embedding_grad_workspace_bytes(ids.numel(), dim, rows) bytes (allocated here when not given)."""
+    g, dim = _rows(grad_out, "grad_out")
+    tokens = _tokens(ids, first_row, _NO_PADDING if padding_id is None else padding_id)
+    if g.rows != tokens.count:
+        raise ValueError("grad_out must have one row for every token")
+    if out is None:
+        if accumulate:
+            raise ValueError("accumulate adds to out, which must be given")
+        out = torch.empty(rows, dim, dtype=grad_out.dtype, device=grad_out.device)
+    o, out_dim = _rows(out, "out")
+    if out_dim != dim or o.rows != rows:
+        raise ValueError("out must have %d rows of grad_out's width" % rows)
+    workspace = _scratch(workspace, mqg_embedding_grad_workspace_bytes(tokens.count, dim, rows), stream, out.device)
+    _one_device([grad_out, ids, out, workspace])
+    st = lib().mqg_embedding_grad(C.byref(g), C.byref(tokens), dim, scale, C.byref(o), 1 if accumulate else 0, workspace.data_ptr(),
+                                  _stream_handle(stream))
+    if st != MQG_OK:
+        raise MqgError(st, "mqg_embedding_grad")
     return out
 
 

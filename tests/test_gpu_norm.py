@@ -1,0 +1,274 @@
+"""The gradient norm and clipping against their definitions in 64 bits and more.
+
+Tolerances.  norm: every square is exact in fp64 and no sum cancels; a value passes through fewer than 300 additions at these
+sizes (32 per piece of a tensor and the pieces of a workgroup, the wave, the workgroup, the partial sums), so the sum is off by
+at most 300 * 2^-53 of itself and the root by half of that and its own rounding: 2e-14.
+Clipping: the factor is rounded to fp32 (2^-24), the product once (2^-24), the result to the output's type (eps / 2), and where
+that type's values are subnormal by half its smallest step."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from oracle import ref
+from paper_1804_08066_amd import mqgrad as mq
+from paper_1804_08066_amd import workloads
+from helpers import to_u32
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+F32, F16, BF16 = torch.float32, torch.float16, torch.bfloat16
+TYPES = [F32, F16, BF16]
+
+
+def values(n, seed, dtype=F32, std=1e-2):
+    return workloads.normal(n, std, seed, DEV).to(dtype)
+
+
+def long(t):
+    return t.detach().cpu().to(torch.float64).numpy().astype(np.longdouble)
+
+
+def exact_norm(tensors):
+    return float(np.sqrt(sum((np.sum(long(t) ** 2) for t in tensors), np.longdouble(0))))
+
+
+def assert_norm(got, tensors):
+    want = exact_norm(tensors)
+    assert got.dtype == torch.float64 and got.numel() == 1
+    assert abs(got.item() - want) <= 2e-14 * want
+
+
+def assert_clipped(out, x, norm, max_norm):
+    c = 1.0 if norm <= max_norm else max_norm / norm
+    want = x.detach().cpu().double().numpy() * c
+    got = out.detach().cpu().double().numpy()
+    info = torch.finfo(out.dtype)
+    tol = 0.0 if out.dtype == F32 else info.eps / 2
+    tol += 0.0 if c == 1.0 else 2.0 ** -23 * 1.001
+    assert got.shape == want.shape
+    assert np.all(np.abs(got - want) <= tol * np.abs(want) * 1.01 + info.smallest_normal * info.eps / 2)
+
+
+SIZES = [[1], [5], [0, 3, 0], [255, 256, 257], [8191, 8192, 8193], [100_003], [3, 0, 40_000, 1, 8192 * 3, 17], [2_000_001, 64, 999_999],
+         [8192 * 2048 + 5]]
+
+
+@pytest.mark.parametrize("sizes", SIZES, ids=lambda s: "-".join(map(str, s)))
+@pytest.mark.parametrize("dtype", TYPES, ids=str)
+def test_norm(dtype, sizes):
+    tensors = [values(n, 7 * k + 1, dtype) for k, n in enumerate(sizes)]
+    got = mq.mqg_global_norm(tensors)
+    assert_norm(got, tensors)
+    again = mq.mqg_global_norm(tensors, workspace=torch.full((mq.mqg_global_norm_workspace_bytes(len(sizes)),), 255, dtype=torch.uint8, device=DEV))
+    assert again.item() == got.item()
+
+
+@pytest.mark.parametrize("out", TYPES, ids=str)
+@pytest.mark.parametrize("dtype", TYPES, ids=str)
+@pytest.mark.parametrize("ratio", [0.3, 5.0])
+def test_clip_into_outputs(dtype, out, ratio):
+    sizes = [1, 8192, 0, 8195, 31, 70_001]
+    tensors = [values(n, 5 * k + 2, dtype) for k, n in enumerate(sizes)]
+    before = [t.clone() for t in tensors]
+    outputs = [torch.full((n,), 7.0, dtype=out, device=DEV) for n in sizes]
+    max_norm = ratio * exact_norm(tensors)
+    got, norm = mq.mqg_clip_global_norm(tensors, max_norm, outputs=outputs)
+    assert got is outputs
+    assert_norm(norm, tensors)
+    for t, b, o in zip(tensors, before, outputs):
+        assert torch.equal(t, b)
+        assert_clipped(o, t, norm.item(), max_norm)
+        if ratio > 1 and dtype == out:
+            assert torch.equal(o, t)
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=str)
+@pytest.mark.parametrize("ratio", [0.01, 0.999, 1.001])
+def test_clip_in_place(dtype, ratio):
+    sizes = [40_000, 3, 8192, 1_000_003]
+    tensors = [values(n, 3 * k + 9, dtype) for k, n in enumerate(sizes)]
+    before = [t.clone() for t in tensors]
+    max_norm = ratio * exact_norm(tensors)
+    outputs, norm = mq.mqg_clip_global_norm(tensors, max_norm)
+    assert all(o is t for o, t in zip(outputs, tensors))
+    for t, b in zip(tensors, before):
+        assert_clipped(t, b, norm.item(), max_norm)
+        if ratio > 1:
+            assert torch.equal(t, b)
+
+
+def test_mixed_types_and_many_tensors():
+    """More tensors than one launch takes, of all types and odd sizes, slices that are aligned to one value only."""
+    rng = np.random.default_rng(3)
+    tensors, outputs = [], []
+    for k in range(401):
+        n = int(rng.choice([0, 1, 7, 100, 8192, 8193, 20_000]))
+        tensors.append(values(n + 1, k, TYPES[k % 3])[1:])
+        outputs.append(torch.zeros(n + 1, dtype=TYPES[(k // 3) % 3], device=DEV)[1:])
+    norm = mq.mqg_global_norm(tensors)
+    assert_norm(norm, tensors)
+    max_norm = 0.37 * norm.item()
+    _, again = mq.mqg_clip_global_norm(tensors, max_norm, outputs=outputs)
+    assert again.item() == norm.item()
+    for t, o in zip(tensors, outputs):
+        assert_clipped(o, t, norm.item(), max_norm)
+    other = [torch.zeros_like(o) for o in outputs]
+    mq.mqg_clip_by_norm(tensors, norm, max_norm, outputs=other)
+    assert all(torch.equal(a, b) for a, b in zip(outputs, other))
+
+
+def test_one_tensor_several_times_counts_several_times():
+    t = values(5000, 4)
+    assert_norm(mq.mqg_global_norm([t, t, t]), [t, t, t])
+    outs = [torch.zeros_like(t), torch.zeros_like(t)]
+    mq.mqg_clip_global_norm([t, t], 0.1, outputs=outs)
+    assert torch.equal(*outs)
+    with pytest.raises(mq.MqgError):
+        mq.mqg_clip_global_norm([t, t], 0.1)     # in place: each would be scaled by the other's call
+
+
+def test_no_values():
+    assert mq.mqg_global_norm([]).item() == 0.0
+    empty = torch.empty(0, device=DEV)
+    assert mq.mqg_global_norm([empty, empty]).item() == 0.0
+    outputs, norm = mq.mqg_clip_global_norm([empty], 1.0)
+    assert norm.item() == 0.0 and outputs[0].numel() == 0
+    zeros = torch.zeros(1000, device=DEV)
+    _, norm = mq.mqg_clip_global_norm([zeros], 0.0)
+    assert norm.item() == 0.0 and not zeros.any()
+
+
+def test_no_square_overflows_or_vanishes():
+    for scale in (1e38, 1e-38, 1e-44):
+        t = torch.full((1000,), scale, device=DEV)
+        assert_norm(mq.mqg_global_norm([t]), [t])
+        _, norm = mq.mqg_clip_global_norm([t], 0.5 * math.sqrt(1000.0) * float(t[0].double()))
+        assert norm.item() > 0
+        assert abs(t.double().max().item() - 0.5 * float(torch.tensor(scale, dtype=F32).double())) <= max(2.0 ** -23 * scale, 2.0 ** -149)
+    t = torch.full((100_000,), 60000.0, dtype=F16, device=DEV)
+    assert_norm(mq.mqg_global_norm([t]), [t])
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=str)
+def test_infinite_and_missing_values_show(dtype):
+    """An infinite norm scales finite values to zero, a norm that is not a number spoils them all; nothing is clipped to infinity."""
+    x = values(9000, 6, dtype)
+    x[5000] = float("inf")
+    out = torch.zeros_like(x)
+    _, norm = mq.mqg_clip_global_norm([x], 1.0, outputs=[out])
+    assert norm.item() == float("inf")
+    assert torch.isnan(out[5000]) and not out[:5000].any() and not out[5001:].any()
+    _, norm = mq.mqg_clip_global_norm([x], float("inf"), outputs=[out])
+    assert norm.item() == float("inf") and torch.equal(out, x)
+    x[17] = float("nan")
+    _, norm = mq.mqg_clip_global_norm([x], float("inf"), outputs=[out])
+    assert math.isnan(norm.item()) and torch.isnan(out).all()
+
+
+def test_only_the_outputs_are_written():
+    flat = torch.full((30_000,), 3.0, device=DEV)
+    tensors = [values(9001, 1, BF16), values(8200, 2, BF16)]
+    mq.mqg_clip_global_norm(tensors, 0.5, outputs=[flat[11:9012], flat[10_000:18_200]])
+    keep = torch.ones(30_000, dtype=torch.bool, device=DEV)
+    keep[11:9012] = False
+    keep[10_000:18_200] = False
+    assert (flat[keep] == 3.0).all() and not (flat[~keep] == 3.0).any()
+
+
+def test_shards_norms_combine():
+    """A model over several GPUs: the square sum of the shards' norms is the model's, and every shard clips by it."""
+    shards = [[values(10_000, 10 * s + k) for k in range(3)] for s in range(4)]
+    norms = torch.cat([mq.mqg_global_norm(s) for s in shards])
+    norm = norms.square().sum().sqrt().view(1)
+    every = [t for s in shards for t in s]
+    assert abs(norm.item() - exact_norm(every)) <= 1e-13 * norm.item()
+    before = [t.clone() for t in every]
+    for s in shards:
+        mq.mqg_clip_by_norm(s, norm, 0.25)
+    for t, b in zip(every, before):
+        assert_clipped(t, b, norm.item(), 0.25)
+
+
+@pytest.mark.parametrize("bits", [1, 4, 7])
+def test_clipped_scales_are_the_clipped_gradients(bits):
+    """Quantized first and clipped by its scales, the stream de-quantizes to c times what it did: both products are fp32."""
+    g = values(50_000, 12)
+    packed, scales = mq.mqg_quantize(g, bits, 512, seed=3)
+    before = mq.mqg_aggregate_mean([packed], [scales], g.numel(), bits, 512)
+    norm = mq.mqg_global_norm([g])
+    mq.mqg_clip_by_norm([scales], norm, 0.5)
+    after = mq.mqg_aggregate_mean([packed], [scales], g.numel(), bits, 512)
+    c = 0.5 / norm.item()
+    assert c < 1.0
+    want = before.double() * c
+    # the factor, the product with the scale, the division by L and the product with the code on either side: 7 roundings
+    assert ((after.double() - want).abs() <= 7 * 2.0 ** -24 * want.abs()).all()
+
+
+def test_other_stream_and_replayed_graph():
+    tensors = [values(100_000, 1, BF16), values(333, 2), values(9000, 3, F16)]
+    outputs = [torch.zeros(t.numel(), device=DEV) for t in tensors]
+    workspace = torch.empty(mq.mqg_global_norm_workspace_bytes(3), dtype=torch.uint8, device=DEV)
+    norm = torch.zeros(1, dtype=torch.float64, device=DEV)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    mq.mqg_clip_global_norm(tensors, 0.1, outputs=outputs, workspace=workspace, norm_out=norm, stream=side)
+    _, fresh = mq.mqg_clip_global_norm(tensors, 0.1, outputs=[torch.zeros_like(o) for o in outputs], stream=side)
+    torch.cuda.current_stream().wait_stream(side)
+    assert norm.item() == fresh.item()
+    assert_norm(norm, tensors)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        mq.mqg_clip_global_norm(tensors, 0.1, outputs=outputs, workspace=workspace, norm_out=norm)
+    for replay in range(4):
+        for k, t in enumerate(tensors):
+            t.copy_(values(t.numel(), 100 * replay + k, t.dtype, std=10.0 ** (replay - 3)))
+        graph.replay()
+        torch.cuda.synchronize()
+        assert_norm(norm, tensors)
+        for t, o in zip(tensors, outputs):
+            assert_clipped(o, t, norm.item(), 0.1)
+
+
+def test_clipped_gradients_through_the_exchange():
+    """Half-precision gradients of two workers, clipped into flat buffers, quantized and applied, against the oracle on the
+    clipped values."""
+    sizes, bits, bucket, lr = [4800, 64, 50_001], 4, 512, 0.1
+    n, W = sum(sizes), 2
+    params = workloads.uniform(n, -0.05, 0.05, 3, DEV)
+    host = params.cpu().numpy().copy()
+    streams, want = [], []
+    for w in range(W):
+        grads = [values(k, 40 * w + i, BF16) for i, k in enumerate(sizes)]
+        flat = torch.empty(n, device=DEV)
+        mq.mqg_clip_global_norm(grads, 0.5, outputs=list(flat.split(sizes)))
+        streams.append(mq.mqg_quantize(flat, bits, bucket, seed=1, worker=w))
+        want.append(ref.quantize(flat.cpu().numpy(), bits, bucket, 1, 0, w))
+        assert abs(exact_norm([flat]) - 0.5) < 1e-4
+    mq.mqg_aggregate_update([s[0] for s in streams], [s[1] for s in streams], n, bits, bucket, lr, params)
+    for (pk, sc), (pk_o, sc_o) in zip(streams, want):
+        assert np.array_equal(to_u32(pk), pk_o) and np.array_equal(sc.cpu().numpy(), sc_o)
+    host = ref.aggregate_update([s[0] for s in want], [s[1] for s in want], n, bits, bucket, lr, host)
+    assert np.array_equal(params.cpu().numpy(), host)
+
+
+def test_binding_refusals():
+    t = values(100, 1)
+    with pytest.raises(TypeError):
+        mq.mqg_global_norm([t, t.double()])
+    with pytest.raises(TypeError):
+        mq.mqg_global_norm([t.view(10, 10).t()])
+    with pytest.raises(TypeError):
+        mq.mqg_global_norm([t], norm_out=torch.zeros(1, device=DEV))
+    with pytest.raises(ValueError):
+        mq.mqg_global_norm([t], workspace=torch.empty(8, dtype=torch.uint8, device=DEV))
+    with pytest.raises(ValueError):
+        mq.mqg_clip_global_norm([t], 1.0, outputs=[t[:50]])
+    with pytest.raises(ValueError):
+        mq.mqg_clip_global_norm([t], 1.0, outputs=[])
+    with pytest.raises(mq.MqgError):
+        mq.mqg_clip_global_norm([t], -1.0)
+    with pytest.raises(mq.MqgError):
+        mq.mqg_clip_global_norm([t[:50]], 1.0, outputs=[t[25:75]])
