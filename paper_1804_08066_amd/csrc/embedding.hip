@@ -4,6 +4,7 @@
 // one row keep their order), and the rows of grad_out that belong to one row of the table are then a run of that order.  No
 // atomic adds a floating value, so equal inputs give equal bits.
 
+#include <algorithm>
 #include <type_traits>
 
 #include "kernels.h"
@@ -31,28 +32,29 @@ __global__ __launch_bounds__(kThreads) void embedding_kernel(const RowMatrix tab
                                                              const float scale, const RowMatrix out) {
     constexpr int V = IN == kF32 || OUT == kF32 ? 4 : 8;
     const uint32_t lane = threadIdx.x & ((1u << shift) - 1u);
-    const uint64_t p = (uint64_t)blockIdx.x * (kThreads >> shift) + (threadIdx.x >> shift);
     const uint32_t col = ((blockIdx.y << shift) + lane) * V;
-    if (p >= ids.count || col >= dim) return;
-    const uint32_t row = row_of<WIDE>(ids, p, table.rows, false);
-    const bool there = row < table.rows;
-    const void* x = at<IN>(table.data, (uint64_t)row * table.stride + col);
-    void* y = at<OUT>(out.data, p * out.stride + col);
-    if (col + V <= dim) {
-        float v[V] = {};
-        if (there) {
-            Pack<IN, V> t;
-            t.load(x);
-            t.get(v);
+    if (col >= dim) return;
+    for (uint64_t p = (uint64_t)blockIdx.x * (kThreads >> shift) + (threadIdx.x >> shift); p < ids.count; p += (uint64_t)gridDim.x * (kThreads >> shift)) {
+        const uint32_t row = row_of<WIDE>(ids, p, table.rows, false);
+        const bool there = row < table.rows;
+        const void* x = at<IN>(table.data, (uint64_t)row * table.stride + col);
+        void* y = at<OUT>(out.data, p * out.stride + col);
+        if (col + V <= dim) {
+            float v[V] = {};
+            if (there) {
+                Pack<IN, V> t;
+                t.load(x);
+                t.get(v);
 #pragma unroll
-            for (int i = 0; i < V; ++i) v[i] *= scale;
+                for (int i = 0; i < V; ++i) v[i] *= scale;
+            }
+            Pack<OUT, V> o;
+            o.set(v);
+            o.store(y);
+        } else {
+            for (uint32_t i = 0; col + i < dim; ++i) store_one<OUT>(y, i, there ? load_one<IN>(x, i) * scale : 0.0f);
         }
-        Pack<OUT, V> o;
-        o.set(v);
-        o.store(y);
-        return;
     }
-    for (uint32_t i = 0; col + i < dim; ++i) store_one<OUT>(y, i, there ? load_one<IN>(x, i) * scale : 0.0f);
 }
 
 // ---- the sort ------------------------------------------------------------------------------------------
@@ -86,6 +88,7 @@ struct SortArgs {
     uint32_t* keys_out;
     uint32_t* order_out;
     uint32_t* counts;         // [ranges][1 << bits]
+    uint4* named;             // first pass of a gradient that is overwritten: [rows] bytes, cleared by the count and set by the scatter
     uint64_t range;
     uint32_t ranges, bits, shift;
 };
@@ -99,6 +102,11 @@ template <bool WIDE>
 __global__ __launch_bounds__(kSortThreads) void sort_count_kernel(const SortArgs a) {
     __shared__ uint32_t s_count[1u << kMaxDigitBits];
     const uint32_t digits = 1u << a.bits;
+    if (a.named != nullptr) {
+        const uint64_t all = (a.rows + 15u) / 16u;
+        for (uint64_t i = (uint64_t)blockIdx.x * kSortThreads + threadIdx.x; i < all; i += (uint64_t)gridDim.x * kSortThreads) a.named[i] = make_uint4(0u, 0u, 0u, 0u);
+    }
+    if (blockIdx.x >= a.ranges) return;
     for (uint32_t d = threadIdx.x; d < digits; d += kSortThreads) s_count[d] = 0u;
     __syncthreads();
     const uint64_t first = (uint64_t)blockIdx.x * a.range, end = min(first + a.range, a.ids.count);
@@ -197,18 +205,13 @@ __global__ __launch_bounds__(kSortThreads) void sort_scatter_kernel(const SortAr
             const uint32_t to = s_wave[wave][(key[j] >> a.shift) & (digits - 1u)] + rank[j];
             a.keys_out[to] = key[j];
             a.order_out[to] = from[j];
+            if (a.named != nullptr && key[j] < a.rows) reinterpret_cast<uint8_t*>(a.named)[key[j]] = 1u;
         }
     }
 }
 
-// ---- the sums ------------------------------------------------------------------------------------------
-template <int OUT>
-__global__ __launch_bounds__(kThreads) void clear_rows_kernel(const RowMatrix out, const uint32_t dim, const uint32_t shift) {
-    constexpr int V = OUT == kF32 ? 4 : 8;
-    const uint32_t lane = threadIdx.x & ((1u << shift) - 1u);
-    const uint64_t row = (uint64_t)blockIdx.x * (kThreads >> shift) + (threadIdx.x >> shift);
-    const uint32_t col = ((blockIdx.y << shift) + lane) * V;
-    if (row >= out.rows || col >= dim) return;
+template <int OUT, int V>
+__device__ __forceinline__ void clear_row(const RowMatrix& out, uint32_t dim, uint64_t row, uint32_t col) {
     void* y = at<OUT>(out.data, row * out.stride + col);
     if (col + V <= dim) {
         const float zero[V] = {};
@@ -219,35 +222,208 @@ __global__ __launch_bounds__(kThreads) void clear_rows_kernel(const RowMatrix ou
     }
     for (uint32_t i = 0; col + i < dim; ++i) store_one<OUT>(y, i, 0.0f);
 }
-
-// The lanes of the first position of a run add up the run.
-template <int IN, int OUT, bool ACCUMULATE>
-__global__ __launch_bounds__(kThreads) void sum_runs_kernel(const uint32_t* __restrict__ keys, const uint32_t* __restrict__ order, const uint64_t count,
-                                                            const RowMatrix grad, const uint32_t dim, const uint32_t shift, const float scale, const RowMatrix out) {
-    constexpr int V = IN == kF32 ? 4 : 8;
+// a table without tokens: all of it is cleared
+template <int OUT>
+__global__ __launch_bounds__(kThreads) void clear_rows_kernel(const RowMatrix out, const uint32_t dim, const uint32_t shift) {
+    constexpr int V = OUT == kF32 ? 4 : 8;
     const uint32_t lane = threadIdx.x & ((1u << shift) - 1u);
-    const uint64_t first = (uint64_t)blockIdx.x * (kThreads >> shift) + (threadIdx.x >> shift);
     const uint32_t col = ((blockIdx.y << shift) + lane) * V;
-    if (first >= count || col >= dim) return;
-    const uint32_t row = keys[first];
-    if (row >= out.rows || (first > 0 && keys[first - 1u] == row)) return;
-    const uint32_t some = col + V <= dim ? V : dim - col;
-    float sum[V] = {};
-    for (uint64_t i = first; i < count && keys[i] == row; ++i) {
-        const void* x = at<IN>(grad.data, (uint64_t)order[i] * grad.stride + col);
-        float v[V] = {};
-        if (some == V) {
-            Pack<IN, V> t;
-            t.load(x);
-            t.get(v);
-        } else {
-            for (uint32_t j = 0; j < some; ++j) v[j] = load_one<IN>(x, j);
+    if (col >= dim) return;
+    for (uint64_t row = (uint64_t)blockIdx.x * (kThreads >> shift) + (threadIdx.x >> shift); row < out.rows; row += (uint64_t)gridDim.x * (kThreads >> shift)) {
+        clear_row<OUT, V>(out, dim, row, col);
+    }
+}
+
+// ---- the sums ------------------------------------------------------------------------------------------
+// The sorted positions are cut into chunks, and the lanes of a chunk add up its runs, eight rows of grad_out in flight.  A run
+// that starts in a chunk and ends in the next one is added up by the chunk it starts in; one that goes on into the chunk after
+// that is long: each of its chunks leaves a partial sum, which join_runs_kernel adds up in the order of the chunks.  So a row
+// of the table that half a batch names is read by as many workgroups as any other half, and every chunk can tell from the
+// keys around it which of its runs are whose.
+constexpr uint32_t kRows = 8;            // in flight
+
+struct SumArgs {
+    const uint32_t *keys, *order;
+    uint64_t count;                       // positions
+    RowMatrix grad, out;
+    float* partials;                      // [chunks][2][width]: of the long run that a chunk begins in, and of the one that begins in it
+    const uint8_t* named;                 // [rows], rows that a position names; nullptr: rows that none names are left as they are
+    uint32_t dim, width, shift, chunk;    // width: dim, rounded up to 8; 1 << shift lanes hold a row or a slice of it
+    uint32_t chunk_blocks;                // workgroups of chunks; the others clear rows
+    float scale;
+    bool accumulate;
+};
+
+// the next chunk's positions [start, ...) continue a run of key `k` that starts before them: is that run long?
+__device__ __forceinline__ bool continues_long(const SumArgs& a, uint64_t start, uint32_t k) {
+    const bool began_before = start > a.chunk && a.keys[start - a.chunk - 1u] == k;
+    return began_before || (start + a.chunk < a.count && a.keys[start + a.chunk] == k);
+}
+
+template <int OUT, int V>
+__device__ __forceinline__ void write_row(const SumArgs& a, uint32_t row, uint32_t col, const float (&sum)[V]) {
+    void* y = at<OUT>(a.out.data, (uint64_t)row * a.out.stride + col);
+    if (col + V <= a.dim) {
+        float v[V];
+        Pack<OUT, V> o;
+        if (a.accumulate) {
+            o.load(y);
+            o.get(v);
         }
 #pragma unroll
-        for (int j = 0; j < V; ++j) sum[j] += v[j];
+        for (int i = 0; i < V; ++i) v[i] = a.accumulate ? __builtin_fmaf(a.scale, sum[i], v[i]) : a.scale * sum[i];
+        o.set(v);
+        o.store(y);
+        return;
     }
-    void* y = at<OUT>(out.data, (uint64_t)row * out.stride + col);
-    for (uint32_t j = 0; j < some; ++j) store_one<OUT>(y, j, ACCUMULATE ? __builtin_fmaf(scale, sum[j], load_one<OUT>(y, j)) : scale * sum[j]);
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+        if (col + i < a.dim) store_one<OUT>(y, i, a.accumulate ? __builtin_fmaf(a.scale, sum[i], load_one<OUT>(y, i)) : a.scale * sum[i]);
+    }
+}
+template <int V>
+__device__ __forceinline__ void write_partial(const SumArgs& a, uint64_t chunk, uint32_t slot, uint32_t col, const float (&sum)[V]) {
+    float* p = a.partials + (2u * chunk + slot) * a.width + col;   // a whole number of V: width is
+    Pack<kF32, V> o;
+    o.set(sum);
+    o.store(p);
+}
+
+// UNIFORM: a wave's lanes all belong to one chunk, whose keys are then scalar loads
+template <int IN, int OUT, bool UNIFORM>
+__global__ __launch_bounds__(kThreads) void sum_runs_kernel(const SumArgs a) {
+    constexpr int V = IN == kF32 ? 4 : 8;
+    const uint32_t lane = threadIdx.x & ((1u << a.shift) - 1u);
+    const uint32_t col = ((blockIdx.y << a.shift) + lane) * V;
+    if (col >= a.dim) return;
+    if (blockIdx.x >= a.chunk_blocks) {
+        uint64_t row = (uint64_t)(blockIdx.x - a.chunk_blocks) * (kThreads >> a.shift) + (threadIdx.x >> a.shift);
+        for (; row < a.out.rows; row += (uint64_t)(gridDim.x - a.chunk_blocks) * (kThreads >> a.shift)) {
+            if (a.named[row] == 0u) clear_row<OUT, V>(a.out, a.dim, row, col);
+        }
+        return;
+    }
+    uint32_t c = blockIdx.x * (kThreads >> a.shift) + (threadIdx.x >> a.shift);
+    if constexpr (UNIFORM) c = (uint32_t)__builtin_amdgcn_readfirstlane((int)c);
+    const uint64_t start = (uint64_t)c * a.chunk, end = min(start + a.chunk, a.count);
+    if (start >= a.count) return;
+    uint32_t cur = a.keys[start];
+    const uint32_t rows = (uint32_t)a.out.rows;
+    if (cur >= rows) return;                               // keys rise: no position from here on adds to a row
+    const uint32_t last = a.keys[end - 1u];                // a run of this key may go on behind the chunk
+    bool skip = false, head = false;                       // of the run that began before this chunk
+    if (start > 0u && a.keys[start - 1u] == cur) {
+        head = continues_long(a, start, cur);
+        skip = !head;
+    }
+    const bool tail = end < a.count && continues_long(a, end, last);   // where the last key's run goes on at all
+    const uint32_t beyond = tail ? rows : last;            // key whose positions behind the chunk belong to it: `rows` for none
+    float sum[V] = {};
+    const auto finish = [&](bool ends) {                   // the run of `cur`, which ends here or goes on behind the chunk
+        if (head) write_partial<V>(a, c, 0u, col, sum);
+        else if (!ends && tail) write_partial<V>(a, c, 1u, col, sum);
+        else if (!skip) write_row<OUT, V>(a, cur, col, sum);
+    };
+    const bool whole = col + V <= a.dim;
+    for (uint64_t i = start;; i += kRows) {
+        uint32_t key[kRows];
+        bool valid[kRows];
+        Pack<IN, V> t[kRows];
+#pragma unroll
+        for (uint32_t j = 0; j < kRows; ++j) {
+            const bool in = i + j < a.count;
+            key[j] = in ? a.keys[i + j] : rows;
+            valid[j] = in && key[j] < rows && (i + j < end || key[j] == beyond);
+        }
+#pragma unroll
+        for (uint32_t j = 0; j < kRows; ++j) {
+            if (!valid[j] || (skip && key[j] == cur)) continue;
+            const void* x = at<IN>(a.grad.data, (uint64_t)a.order[i + j] * a.grad.stride + col);
+            if (whole) {
+                t[j].load(x);
+            } else {
+                float v[V];
+#pragma unroll
+                for (int l = 0; l < V; ++l) v[l] = col + l < a.dim ? load_one<IN>(x, l) : 0.0f;
+                t[j].set(v);
+            }
+        }
+#pragma unroll
+        for (uint32_t j = 0; j < kRows; ++j) {
+            if (!valid[j]) {
+                finish(i + j < end || key[j] != last);
+                return;
+            }
+            if (key[j] != cur) {
+                finish(true);
+                cur = key[j];
+                head = skip = false;
+#pragma unroll
+                for (int l = 0; l < V; ++l) sum[l] = 0.0f;
+            }
+            if (!skip) {
+                float v[V];
+                t[j].get(v);
+#pragma unroll
+                for (int l = 0; l < V; ++l) sum[l] += v[l];
+            }
+        }
+    }
+}
+
+// The partial sums of the long run that begins in a chunk: the waves take them in turn, and add up theirs in order.
+constexpr uint32_t kJoinWaves = 8, kJoinThreads = 64u * kJoinWaves;
+template <int OUT>
+__global__ __launch_bounds__(kJoinThreads) void join_runs_kernel(const SumArgs a) {
+    __shared__ float s_sum[kJoinWaves][64][4];
+    const uint64_t c = blockIdx.x, start = c * a.chunk, end = start + a.chunk;
+    if (end >= a.count) return;
+    const uint32_t k = a.keys[end];
+    if (k >= a.out.rows || a.keys[end - 1u] != k || (start > 0u && a.keys[start - 1u] == k) || !continues_long(a, end, k)) return;
+    const uint32_t lane = threadIdx.x & 63u, wave = threadIdx.x >> 6, col = (blockIdx.y * 64u + lane) * 4u;
+    // chunks behind this one that begin in the run: a search by 64 at a time
+    const uint64_t most = (a.count - 1u) / a.chunk - c;
+    uint64_t low = 2, high = most + 1u;                    // chunk c + low - 1 begins in it, chunk c + high does not
+    while (low < high) {
+        const uint64_t step = (high - low + 63u) / 64u, probe = low + lane * step;
+        const bool in = probe < high && a.keys[(c + probe) * a.chunk] == k;
+        const uint32_t seen = (uint32_t)__builtin_popcountll(__builtin_amdgcn_ballot_w64(in));
+        if (seen == 0u) break;
+        const uint64_t found = low + (uint64_t)(seen - 1u) * step;   // begins in it
+        high = min(high, found + step);
+        low = found + 1u;
+    }
+    const uint64_t parts = low;                            // slot 1 of c, slot 0 of c + 1 .. c + low - 1
+    float sum[4] = {};
+    if (col < a.width) {
+        constexpr uint32_t kAhead = 4;
+        for (uint64_t p = wave; p < parts; p += kAhead * kJoinWaves) {
+            Pack<kF32, 4> t[kAhead];
+#pragma unroll
+            for (uint32_t j = 0; j < kAhead; ++j) {
+                const uint64_t q = p + j * kJoinWaves;
+                if (q < parts) t[j].load(a.partials + (2u * (c + q) + (q == 0u ? 1u : 0u)) * a.width + col);
+            }
+#pragma unroll
+            for (uint32_t j = 0; j < kAhead; ++j) {
+                if (p + j * kJoinWaves >= parts) continue;
+                float v[4];
+                t[j].get(v);
+#pragma unroll
+                for (int l = 0; l < 4; ++l) sum[l] += v[l];
+            }
+        }
+    }
+#pragma unroll
+    for (int l = 0; l < 4; ++l) s_sum[wave][lane][l] = sum[l];
+    __syncthreads();
+    if (wave != 0u || col >= a.dim) return;
+#pragma unroll
+    for (uint32_t w = 1; w < kJoinWaves; ++w) {
+#pragma unroll
+        for (int l = 0; l < 4; ++l) sum[l] += s_sum[w][lane][l];
+    }
+    write_row<OUT, 4>(a, k, col, sum);
 }
 
 // lanes that hold a row, as a power of two of at most a workgroup, and slices of a row
@@ -256,17 +432,30 @@ uint32_t row_shift(uint32_t dim, uint32_t v) {
     while ((1u << shift) < kThreads && (1u << shift) * v < dim) ++shift;
     return shift;
 }
+constexpr uint64_t kMaxBlocks = 1u << 22;   // a launch holds less than 2^32 lanes: the workgroups take rows in turn from there on
 dim3 row_grid(uint64_t rows, uint32_t dim, uint32_t v) {
     const uint32_t shift = row_shift(dim, v), per = kThreads >> shift, width = v << shift;
-    return dim3((uint32_t)((rows + per - 1u) / per), (dim + width - 1u) / width);
+    return dim3((uint32_t)std::min<uint64_t>((rows + per - 1u) / per, kMaxBlocks), (dim + width - 1u) / width);
+}
+
+// Positions of a chunk: enough chunks to fill the GPU, as long as that allows (a long run leaves a partial sum in every chunk).
+uint32_t chunk_of(uint64_t tokens, uint32_t dim) {
+    const uint64_t waves = tokens * ((dim + 511u) / 512u);
+    uint32_t chunk = 8;
+    while (chunk < 64u && waves / (2u * chunk) >= 4096u) chunk *= 2u;
+    while (tokens / chunk >= kMaxBlocks) chunk *= 2u;
+    return chunk;
 }
 
 struct GradWorkspace {
-    uint32_t *keys[2], *order[2], *counts;
+    uint32_t *keys[2], *order[2], *counts, *named;
+    float* partials;
     size_t bytes;
 };
-GradWorkspace grad_workspace(void* base, uint64_t tokens, uint64_t rows) {
+GradWorkspace grad_workspace(void* base, uint64_t tokens, uint32_t dim, uint64_t rows) {
     GradWorkspace w = {};
+    w.named = static_cast<uint32_t*>(base);
+    w.bytes = (rows + 15u) & ~(uint64_t)15u;
     if (tokens == 0) return w;
     const SortShape s = sort_shape(tokens, rows);
     char* p = static_cast<char*>(base);
@@ -280,6 +469,8 @@ GradWorkspace grad_workspace(void* base, uint64_t tokens, uint64_t rows) {
         w.order[i] = take(tokens);
     }
     w.counts = take((uint64_t)s.ranges << s.bits);
+    const uint32_t chunk = chunk_of(tokens, dim);
+    w.partials = reinterpret_cast<float*>(take((tokens + chunk - 1u) / chunk * 2u * ((dim + 7u) & ~7u)));
     return w;
 }
 
@@ -299,20 +490,28 @@ hipError_t launch_embedding(const RowMatrix& table, const TokenIds& ids, uint32_
     return hipGetLastError();
 }
 
-size_t embedding_grad_workspace(uint64_t tokens, uint32_t dim, uint64_t rows) { return grad_workspace(nullptr, tokens, rows).bytes; }
+size_t embedding_grad_workspace(uint64_t tokens, uint32_t dim, uint64_t rows) { return tokens == 0 ? 0 : grad_workspace(nullptr, tokens, dim, rows).bytes; }
 
 hipError_t launch_embedding_grad(const RowMatrix& grad_out, const TokenIds& ids, uint32_t dim, float scale, const RowMatrix& table_grad,
                                  bool accumulate, void* workspace, hipStream_t stream) {
+    SumArgs b = {};
+    b.count = ids.count;
+    b.grad = grad_out;
+    b.out = table_grad;
+    b.dim = dim;
+    b.width = (dim + 7u) & ~7u;
+    b.scale = scale;
+    b.accumulate = accumulate;
     hipError_t e = hipSuccess;
-    if (!accumulate) {
+    if (ids.count == 0) {
+        if (accumulate) return e;
         with_dtype(table_grad.dtype, [&](auto o) {
             constexpr uint32_t v = o == kF32 ? 4u : 8u;
             hipLaunchKernelGGL((clear_rows_kernel<o>), row_grid(table_grad.rows, dim, v), dim3(kThreads), 0, stream, table_grad, dim, row_shift(dim, v));
         });
-        e = hipGetLastError();
+        return hipGetLastError();
     }
-    if (e != hipSuccess || ids.count == 0) return e;
-    const GradWorkspace w = grad_workspace(workspace, ids.count, table_grad.rows);
+    const GradWorkspace w = grad_workspace(workspace, ids.count, dim, table_grad.rows);
     const SortShape s = sort_shape(ids.count, table_grad.rows);
     SortArgs a = {};
     a.ids = ids;
@@ -321,23 +520,41 @@ hipError_t launch_embedding_grad(const RowMatrix& grad_out, const TokenIds& ids,
     a.range = s.range;
     a.ranges = s.ranges;
     a.bits = s.bits;
+    a.named = accumulate ? nullptr : reinterpret_cast<uint4*>(w.named);
     for (uint32_t pass = 0; pass < s.passes; ++pass) {
         a.keys_out = w.keys[pass & 1u];
         a.order_out = w.order[pass & 1u];
         a.shift = pass * s.bits;
-        hipLaunchKernelGGL((ids.wide ? sort_count_kernel<true> : sort_count_kernel<false>), dim3(s.ranges), dim3(kSortThreads), 0, stream, a);
+        const uint64_t clearing = a.named == nullptr ? 0 : a.rows / (64u * kSortThreads);   // four 16-byte stores a lane
+        const uint32_t count_blocks = (uint32_t)std::max<uint64_t>(s.ranges, std::min<uint64_t>(clearing, 2048));
+        hipLaunchKernelGGL((ids.wide ? sort_count_kernel<true> : sort_count_kernel<false>), dim3(count_blocks), dim3(kSortThreads), 0, stream, a);
         hipLaunchKernelGGL((ids.wide ? sort_scatter_kernel<true> : sort_scatter_kernel<false>), dim3(s.ranges), dim3(kSortThreads), 0, stream, a);
         e = hipGetLastError();
         if (e != hipSuccess) return e;
         a.keys = a.keys_out;
         a.order = a.order_out;
+        a.named = nullptr;
     }
+    b.keys = a.keys;
+    b.order = a.order;
+    b.partials = w.partials;
+    b.named = accumulate ? nullptr : reinterpret_cast<const uint8_t*>(w.named);
+    b.chunk = chunk_of(ids.count, dim);
+    const uint64_t chunks = (ids.count + b.chunk - 1u) / b.chunk;
     with_dtype(grad_out.dtype, [&](auto in) {
         with_dtype(table_grad.dtype, [&](auto o) {
             constexpr uint32_t v = in == kF32 ? 4u : 8u;
-            hipLaunchKernelGGL((accumulate ? sum_runs_kernel<in, o, true> : sum_runs_kernel<in, o, false>), row_grid(ids.count, dim, v), dim3(kThreads), 0, stream,
-                               a.keys, a.order, ids.count, grad_out, dim, row_shift(dim, v), scale, table_grad);
+            b.shift = row_shift(dim, v);
+            dim3 grid = row_grid(chunks, dim, v);
+            b.chunk_blocks = grid.x;
+            if (!accumulate) grid.x += row_grid(b.out.rows, dim, v).x;
+            hipLaunchKernelGGL((b.shift >= 6u ? sum_runs_kernel<in, o, true> : sum_runs_kernel<in, o, false>), grid, dim3(kThreads), 0, stream, b);
         });
+    });
+    e = hipGetLastError();
+    if (e != hipSuccess || chunks < 3u) return e;   // a long run touches three chunks
+    with_dtype(table_grad.dtype, [&](auto o) {
+        hipLaunchKernelGGL((join_runs_kernel<o>), dim3((uint32_t)chunks, (b.width + 255u) / 256u), dim3(kJoinThreads), 0, stream, b);
     });
     return hipGetLastError();
 }
