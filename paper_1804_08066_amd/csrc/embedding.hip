@@ -10,6 +10,7 @@
 #include "kernels.h"
 #include "values.h"
 
+
 namespace mqg {
 namespace {
 
@@ -25,44 +26,108 @@ __device__ __forceinline__ uint32_t row_of(const TokenIds& t, uint64_t i, uint64
     return row < rows && !(padding && id == t.padding) ? (uint32_t)row : (uint32_t)rows;
 }
 
+// Values of a row that a lane holds: 16 bytes of the wider type, which are whole lines for a wave.  (Eight values of which
+// fp32 are two stores of half a line each: the sums of 131072 half-precision rows took 386 us instead of 345.)
+constexpr int values_of(int in, int out) { return in == kF32 || out == kF32 ? 4 : 8; }
+
+// y[0 .. min(V, left)) <- v; once: with streaming stores
+template <int OUT, int V>
+__device__ __forceinline__ void store_values(void* y, const float (&v)[V], uint32_t left, bool once) {
+    if (left >= V) {
+        Pack<OUT, V> o;
+        o.set(v);
+        if (once) o.store_once(y);
+        else o.store(y);
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+        if ((uint32_t)i < left) store_one<OUT>(y, i, v[i]);
+    }
+}
+
 // ---- lookup ------------------------------------------------------------------------------------------
-// `1 << shift` lanes hold a row's (or a slice of a row's) values, V each; blockIdx.y: the slice.
+// `1 << shift` lanes hold a row's (or a slice of a row's) values, V each, of kLookups rows at a time; the slices of a row
+// are neighbouring workgroups, so that rows are read and written as a whole (all first slices first: half the memory channels
+// of rows of 8 KB).  Bound by the fabric between the caches and memory.  The rows are written with streaming stores: they are read next by another kernel,
+// mostly from memory, and stores that stay in the caches push the table out of them.
+constexpr uint32_t kLookups = 2;
 template <int IN, int OUT, bool WIDE>
 __global__ __launch_bounds__(kThreads) void embedding_kernel(const RowMatrix table, const TokenIds ids, const uint32_t dim, const uint32_t shift,
-                                                             const float scale, const RowMatrix out) {
-    constexpr int V = IN == kF32 || OUT == kF32 ? 4 : 8;
-    const uint32_t lane = threadIdx.x & ((1u << shift) - 1u);
-    const uint32_t col = ((blockIdx.y << shift) + lane) * V;
+                                                             const uint32_t slices, const float scale, const RowMatrix out) {
+    constexpr int V = values_of(IN, OUT);
+    const uint32_t lane = threadIdx.x & ((1u << shift) - 1u), per = kThreads >> shift, block = blockIdx.x / slices;
+    const uint32_t col = (((blockIdx.x - block * slices) << shift) + lane) * V;
     if (col >= dim) return;
-    for (uint64_t p = (uint64_t)blockIdx.x * (kThreads >> shift) + (threadIdx.x >> shift); p < ids.count; p += (uint64_t)gridDim.x * (kThreads >> shift)) {
-        const uint32_t row = row_of<WIDE>(ids, p, table.rows, false);
-        const bool there = row < table.rows;
-        const void* x = at<IN>(table.data, (uint64_t)row * table.stride + col);
-        void* y = at<OUT>(out.data, p * out.stride + col);
-        if (col + V <= dim) {
-            float v[V] = {};
-            if (there) {
-                Pack<IN, V> t;
-                t.load(x);
-                t.get(v);
+    const bool whole = col + V <= dim;
+    const uint64_t step = (uint64_t)per * kLookups;
+    for (uint64_t p = block * step + (threadIdx.x >> shift); p < ids.count; p += gridDim.x / slices * step) {
+        uint32_t row[kLookups];
+        bool there[kLookups];
+        Pack<IN, V> t[kLookups] = {};
 #pragma unroll
-                for (int i = 0; i < V; ++i) v[i] *= scale;
-            }
-            Pack<OUT, V> o;
-            o.set(v);
-            o.store(y);
-        } else {
-            for (uint32_t i = 0; col + i < dim; ++i) store_one<OUT>(y, i, there ? load_one<IN>(x, i) * scale : 0.0f);
+        for (uint32_t r = 0; r < kLookups; ++r) {
+            row[r] = p + r * per < ids.count ? row_of<WIDE>(ids, p + r * per, table.rows, false) : (uint32_t)table.rows;
+            there[r] = row[r] < table.rows;
+        }
+#pragma unroll
+        for (uint32_t r = 0; r < kLookups; ++r) {
+            if (!there[r]) continue;
+            const void* x = at<IN>(table.data, (uint64_t)row[r] * table.stride + col);
+            if (whole) t[r].load(x);
+            else t[r].load_some(x, dim - col);
+        }
+#pragma unroll
+        for (uint32_t r = 0; r < kLookups; ++r) {
+            if (p + r * per >= ids.count) break;
+            void* y = at<OUT>(out.data, (p + r * per) * out.stride + col);
+            float v[V];
+            t[r].get(v);
+#pragma unroll
+            for (int i = 0; i < V; ++i) v[i] = there[r] ? v[i] * scale : 0.0f;
+            store_values<OUT>(y, v, dim - col, true);
         }
     }
 }
 
+// ---- rows that become zero ----------------------------------------------------------------------------
+// rows [first, end) are cleared, those that a position names (named[r] != 0) excepted; named == nullptr: all of them
+struct ClearRows {
+    RowMatrix out;
+    const uint8_t* named;
+    uint64_t first, end;
+    uint32_t dim, shift;    // 1 << shift lanes hold a row or a slice of it
+    uint32_t slices;
+};
+template <int OUT>
+__device__ __forceinline__ void clear_rows(const ClearRows& c, uint32_t block, uint32_t blocks) {
+    constexpr int V = OUT == kF32 ? 4 : 8;
+    const uint32_t lane = threadIdx.x & ((1u << c.shift) - 1u), per = blockDim.x >> c.shift;
+    const float zero[V] = {};
+    for (uint64_t row = c.first + (uint64_t)block * per + (threadIdx.x >> c.shift); row < c.end; row += (uint64_t)blocks * per) {
+        if (c.named != nullptr && c.named[row] != 0u) continue;
+        for (uint32_t s = 0; s < c.slices; ++s) {
+            const uint32_t col = ((s << c.shift) + lane) * V;
+            if (col < c.dim) store_values<OUT>(at<OUT>(c.out.data, row * c.out.stride + col), zero, c.dim - col, true);
+        }
+    }
+}
+__device__ __forceinline__ void clear_rows(const ClearRows& c, uint32_t block, uint32_t blocks) {
+    if (c.first < c.end) with_dtype(c.out.dtype, [&](auto o) { clear_rows<o>(c, block, blocks); });
+}
+
+__global__ __launch_bounds__(kThreads) void clear_rows_kernel(const ClearRows c) { clear_rows(c, blockIdx.x, gridDim.x); }
+
 // ---- the sort ------------------------------------------------------------------------------------------
 // Least significant digit first.  Every workgroup owns a range of the positions; a pass counts each range's digits, and the
-// scatter adds up the counts before its own (of smaller digits, and of equal ones in earlier ranges) by itself.
-constexpr uint32_t kSortThreads = 256, kSortWaves = kSortThreads / 64u, kSortItems = 8, kSortTile = kSortThreads * kSortItems;
-constexpr uint32_t kMaxRanges = 256;     // every workgroup reads all ranges' counts: a few, of any length
-constexpr uint32_t kMaxDigitBits = 10;
+// scatter adds up the counts before its own (of smaller digits, and of equal ones in earlier ranges) by itself.  The sort of a
+// batch is a handful of workgroups that wait for memory, so the launches clear rows of the table beside it.
+constexpr uint32_t kSortThreads = 512, kSortWaves = kSortThreads / 64u, kSortItems = 4, kSortTile = kSortThreads * kSortItems;
+constexpr uint32_t kMaxRanges = 128;     // every workgroup reads all ranges' counts: a few, of any length
+constexpr uint32_t kMaxDigitBits = 10, kMaxDigits = 1u << kMaxDigitBits;
+
+constexpr uint64_t kClearBeside = 50000000;   // bytes
+constexpr uint32_t kClearBlocks = 2048;          // what the GPU holds, twice over
 
 struct SortShape {
     uint32_t passes, bits, ranges;
@@ -88,7 +153,8 @@ struct SortArgs {
     uint32_t* keys_out;
     uint32_t* order_out;
     uint32_t* counts;         // [ranges][1 << bits]
-    uint4* named;             // first pass of a gradient that is overwritten: [rows] bytes, cleared by the count and set by the scatter
+    uint4* named;             // first pass, where rows are cleared: [rows] bytes, zeroed by the count and set by the scatter
+    uint32_t* join_count;     // first pass: cleared by the count
     uint64_t range;
     uint32_t ranges, bits, shift;
 };
@@ -99,42 +165,79 @@ __device__ __forceinline__ uint32_t sort_key(const SortArgs& a, uint64_t i) {
 }
 
 template <bool WIDE>
-__global__ __launch_bounds__(kSortThreads) void sort_count_kernel(const SortArgs a) {
-    __shared__ uint32_t s_count[1u << kMaxDigitBits];
+__global__ __launch_bounds__(kSortThreads) void sort_count_kernel(const SortArgs a, const ClearRows c) {
+    __shared__ uint32_t s_count[kMaxDigits];
     const uint32_t digits = 1u << a.bits;
+    if (a.keys == nullptr && blockIdx.x == 0u && threadIdx.x == 0u) *a.join_count = 0u;
     if (a.named != nullptr) {
         const uint64_t all = (a.rows + 15u) / 16u;
         for (uint64_t i = (uint64_t)blockIdx.x * kSortThreads + threadIdx.x; i < all; i += (uint64_t)gridDim.x * kSortThreads) a.named[i] = make_uint4(0u, 0u, 0u, 0u);
     }
-    if (blockIdx.x >= a.ranges) return;
+    if (blockIdx.x >= a.ranges) {
+        clear_rows(c, blockIdx.x - a.ranges, gridDim.x - a.ranges);
+        return;
+    }
     for (uint32_t d = threadIdx.x; d < digits; d += kSortThreads) s_count[d] = 0u;
     __syncthreads();
     const uint64_t first = (uint64_t)blockIdx.x * a.range, end = min(first + a.range, a.ids.count);
-    for (uint64_t i = first + threadIdx.x; i < end; i += kSortThreads) atomicAdd(&s_count[(sort_key<WIDE>(a, i) >> a.shift) & (digits - 1u)], 1u);
+    for (uint64_t tile = first; tile < end; tile += kSortTile) {
+        uint32_t key[kSortItems];
+#pragma unroll
+        for (uint32_t j = 0; j < kSortItems; ++j) {
+            const uint64_t i = tile + j * kSortThreads + threadIdx.x;
+            if (i < end) key[j] = sort_key<WIDE>(a, i);
+        }
+#pragma unroll
+        for (uint32_t j = 0; j < kSortItems; ++j) {
+            if (tile + j * kSortThreads + threadIdx.x < end) atomicAdd(&s_count[(key[j] >> a.shift) & (digits - 1u)], 1u);
+        }
+    }
     __syncthreads();
     for (uint32_t d = threadIdx.x; d < digits; d += kSortThreads) a.counts[(uint64_t)blockIdx.x * digits + d] = s_count[d];
 }
 
 template <bool WIDE>
-__global__ __launch_bounds__(kSortThreads) void sort_scatter_kernel(const SortArgs a) {
-    __shared__ uint32_t s_next[1u << kMaxDigitBits];                    // where the next key of a digit goes
-    __shared__ uint32_t s_wave[kSortWaves][1u << kMaxDigitBits];
+__global__ __launch_bounds__(kSortThreads) void sort_scatter_kernel(const SortArgs a, const ClearRows c) {
+    __shared__ uint32_t s_next[kMaxDigits];                             // where the next key of a digit goes
+    __shared__ uint32_t s_wave[kSortWaves][kMaxDigits];
     __shared__ uint32_t s_total[kSortWaves];
+    if (blockIdx.x >= a.ranges) {
+        clear_rows(c, blockIdx.x - a.ranges, gridDim.x - a.ranges);
+        return;
+    }
     const uint32_t digits = 1u << a.bits, tid = threadIdx.x, lane = tid & 63u, wave = tid >> 6;
 
-    // the keys of smaller digits, and of the same digit in earlier ranges; digits of a thread are consecutive
-    const uint32_t per = (digits + kSortThreads - 1u) / kSortThreads;   // 1, 2 or 4
-    uint32_t before[4] = {}, all[4] = {}, mine = 0;
-    for (uint32_t j = 0; j < per; ++j) {
-        const uint32_t d = tid * per + j;
-        if (d >= digits) break;
-        for (uint32_t r = 0; r < a.ranges; ++r) {
-            const uint32_t c = a.counts[(uint64_t)r * digits + d];
-            if (r < blockIdx.x) before[j] += c;
-            all[j] += c;
+    // the keys of a digit in all ranges, and in the earlier ones; the threads share the ranges out where digits are fewer
+    for (uint32_t d = tid; d < 2u * digits; d += kSortThreads) (d < digits ? s_next : s_wave[0])[d & (digits - 1u)] = 0u;
+    __syncthreads();
+    {
+        const uint32_t shares = digits < kSortThreads ? kSortThreads / digits : 1u;
+        for (uint32_t d0 = tid; d0 < digits * shares; d0 += kSortThreads) {
+            const uint32_t d = d0 & (digits - 1u), share = d0 >> a.bits;
+            uint32_t before = 0, all = 0;
+            constexpr uint32_t kAhead = 16;
+            for (uint32_t r0 = share; r0 < a.ranges; r0 += kAhead * shares) {
+                uint32_t n[kAhead];
+#pragma unroll
+                for (uint32_t j = 0; j < kAhead; ++j) {
+                    const uint32_t r = r0 + j * shares;
+                    n[j] = r < a.ranges ? a.counts[(uint64_t)r * digits + d] : 0u;
+                }
+#pragma unroll
+                for (uint32_t j = 0; j < kAhead; ++j) {
+                    all += n[j];
+                    before += r0 + j * shares < blockIdx.x ? n[j] : 0u;
+                }
+            }
+            atomicAdd(&s_next[d], before);
+            atomicAdd(&s_wave[0][d], all);
         }
-        mine += all[j];
     }
+    __syncthreads();
+    // the keys of smaller digits: every thread adds up consecutive digits
+    const uint32_t per = (digits + kSortThreads - 1u) / kSortThreads;   // 1 or 2
+    uint32_t mine = 0;
+    for (uint32_t j = 0; j < per; ++j) mine += tid * per + j < digits ? s_wave[0][tid * per + j] : 0u;
     uint32_t upto = mine;
 #pragma unroll
     for (uint32_t m = 1; m < 64u; m <<= 1) {
@@ -148,15 +251,12 @@ __global__ __launch_bounds__(kSortThreads) void sort_scatter_kernel(const SortAr
     for (uint32_t j = 0; j < per; ++j) {
         const uint32_t d = tid * per + j;
         if (d >= digits) break;
-        s_next[d] = at + before[j];
-        at += all[j];
+        s_next[d] += at;
+        at += s_wave[0][d];
     }
 
     const uint64_t first = (uint64_t)blockIdx.x * a.range, end = min(first + a.range, a.ids.count);
     for (uint64_t tile = first; tile < end; tile += kSortTile) {
-        __syncthreads();
-        for (uint32_t d = lane; d < digits; d += 64u) s_wave[wave][d] = 0u;
-        __builtin_amdgcn_wave_barrier();
         uint32_t key[kSortItems], from[kSortItems], rank[kSortItems];
         bool valid[kSortItems];
 #pragma unroll
@@ -166,6 +266,9 @@ __global__ __launch_bounds__(kSortThreads) void sort_scatter_kernel(const SortAr
             key[j] = valid[j] ? sort_key<WIDE>(a, i) : 0u;
             from[j] = valid[j] && a.order != nullptr ? a.order[i] : (uint32_t)i;
         }
+        __syncthreads();
+        for (uint32_t d = lane; d < digits; d += 64u) s_wave[wave][d] = 0u;
+        __builtin_amdgcn_wave_barrier();
 #pragma unroll
         for (uint32_t j = 0; j < kSortItems; ++j) {
             const uint32_t d = (key[j] >> a.shift) & (digits - 1u);
@@ -177,10 +280,8 @@ __global__ __launch_bounds__(kSortThreads) void sort_scatter_kernel(const SortAr
             }
             const uint32_t below = __builtin_amdgcn_mbcnt_hi((uint32_t)(same >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)same, 0u));
             uint32_t seen = 0;
-            if (valid[j]) {
-                seen = __hip_atomic_load(&s_wave[wave][d], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WAVEFRONT);
-            }
-            __builtin_amdgcn_wave_barrier();
+            if (valid[j]) seen = __hip_atomic_load(&s_wave[wave][d], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WAVEFRONT);
+            __builtin_amdgcn_wave_barrier();   // a wave's LDS operations keep their order: all have read before one writes
             if (valid[j] && below == 0u) {
                 __hip_atomic_store(&s_wave[wave][d], seen + (uint32_t)__builtin_popcountll(same), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WAVEFRONT);
             }
@@ -192,9 +293,9 @@ __global__ __launch_bounds__(kSortThreads) void sort_scatter_kernel(const SortAr
             uint32_t next = s_next[d];
 #pragma unroll
             for (uint32_t w = 0; w < kSortWaves; ++w) {
-                const uint32_t c = s_wave[w][d];
+                const uint32_t n = s_wave[w][d];
                 s_wave[w][d] = next;
-                next += c;
+                next += n;
             }
             s_next[d] = next;
         }
@@ -210,245 +311,239 @@ __global__ __launch_bounds__(kSortThreads) void sort_scatter_kernel(const SortAr
     }
 }
 
-template <int OUT, int V>
-__device__ __forceinline__ void clear_row(const RowMatrix& out, uint32_t dim, uint64_t row, uint32_t col) {
-    void* y = at<OUT>(out.data, row * out.stride + col);
-    if (col + V <= dim) {
-        const float zero[V] = {};
-        Pack<OUT, V> o;
-        o.set(zero);
-        o.store(y);
-        return;
-    }
-    for (uint32_t i = 0; col + i < dim; ++i) store_one<OUT>(y, i, 0.0f);
-}
-// a table without tokens: all of it is cleared
-template <int OUT>
-__global__ __launch_bounds__(kThreads) void clear_rows_kernel(const RowMatrix out, const uint32_t dim, const uint32_t shift) {
-    constexpr int V = OUT == kF32 ? 4 : 8;
-    const uint32_t lane = threadIdx.x & ((1u << shift) - 1u);
-    const uint32_t col = ((blockIdx.y << shift) + lane) * V;
-    if (col >= dim) return;
-    for (uint64_t row = (uint64_t)blockIdx.x * (kThreads >> shift) + (threadIdx.x >> shift); row < out.rows; row += (uint64_t)gridDim.x * (kThreads >> shift)) {
-        clear_row<OUT, V>(out, dim, row, col);
-    }
-}
-
 // ---- the sums ------------------------------------------------------------------------------------------
 // The sorted positions are cut into chunks, and the lanes of a chunk add up its runs, eight rows of grad_out in flight.  A run
 // that starts in a chunk and ends in the next one is added up by the chunk it starts in; one that goes on into the chunk after
 // that is long: each of its chunks leaves a partial sum, which join_runs_kernel adds up in the order of the chunks.  So a row
 // of the table that half a batch names is read by as many workgroups as any other half, and every chunk can tell from the
-// keys around it which of its runs are whose.
-constexpr uint32_t kRows = 8;            // in flight
+// keys around it which of its runs are whose.  The keys and the order around a workgroup's chunks are in LDS before the first
+// row is asked for: loaded where they are needed, each of them waits for the loads and stores before it (131072 tokens of
+// 4096 half-precision values into fp32: 457 -> 386 us; with 16-byte stores of whole lines and streaming loads 326, 5.1 TB/s of
+// the rows read and written).
+constexpr uint32_t kRows = 8;         // in flight
+constexpr uint32_t kMostChunk = 64, kMostPositions = 2048;   // of a chunk, and of a workgroup's chunks together
 
 struct SumArgs {
     const uint32_t *keys, *order;
     uint64_t count;                       // positions
     RowMatrix grad, out;
     float* partials;                      // [chunks][2][width]: of the long run that a chunk begins in, and of the one that begins in it
-    const uint8_t* named;                 // [rows], rows that a position names; nullptr: rows that none names are left as they are
-    uint32_t dim, width, shift, chunk;    // width: dim, rounded up to 8; 1 << shift lanes hold a row or a slice of it
-    uint32_t chunk_blocks;                // workgroups of chunks; the others clear rows
+    uint2* joins;                         // the long runs, in any order: the chunk that one begins in, and its partial sums
+    uint32_t* join_count;
+    uint32_t dim, width, chunk;           // width: dim, rounded up to 8
+    uint32_t shift, slices;               // 1 << shift lanes hold a row, or one of its slices
     float scale;
     bool accumulate;
 };
 
-// the next chunk's positions [start, ...) continue a run of key `k` that starts before them: is that run long?
-__device__ __forceinline__ bool continues_long(const SumArgs& a, uint64_t start, uint32_t k) {
-    const bool began_before = start > a.chunk && a.keys[start - a.chunk - 1u] == k;
-    return began_before || (start + a.chunk < a.count && a.keys[start + a.chunk] == k);
-}
-
 template <int OUT, int V>
 __device__ __forceinline__ void write_row(const SumArgs& a, uint32_t row, uint32_t col, const float (&sum)[V]) {
     void* y = at<OUT>(a.out.data, (uint64_t)row * a.out.stride + col);
-    if (col + V <= a.dim) {
-        float v[V];
+    const uint32_t left = a.dim - col;
+    float v[V];
+    if (a.accumulate) {
         Pack<OUT, V> o;
-        if (a.accumulate) {
-            o.load(y);
-            o.get(v);
-        }
+        if (left >= V) o.load(y);
+        else o.load_some(y, left);
+        o.get(v);
 #pragma unroll
-        for (int i = 0; i < V; ++i) v[i] = a.accumulate ? __builtin_fmaf(a.scale, sum[i], v[i]) : a.scale * sum[i];
-        o.set(v);
-        o.store(y);
-        return;
-    }
+        for (int i = 0; i < V; ++i) v[i] = __builtin_fmaf(a.scale, sum[i], v[i]);
+    } else {
 #pragma unroll
-    for (int i = 0; i < V; ++i) {
-        if (col + i < a.dim) store_one<OUT>(y, i, a.accumulate ? __builtin_fmaf(a.scale, sum[i], load_one<OUT>(y, i)) : a.scale * sum[i]);
+        for (int i = 0; i < V; ++i) v[i] = a.scale * sum[i];
     }
-}
-template <int V>
-__device__ __forceinline__ void write_partial(const SumArgs& a, uint64_t chunk, uint32_t slot, uint32_t col, const float (&sum)[V]) {
-    float* p = a.partials + (2u * chunk + slot) * a.width + col;   // a whole number of V: width is
-    Pack<kF32, V> o;
-    o.set(sum);
-    o.store(p);
+        store_values<OUT>(y, v, left, !a.accumulate);
 }
 
-// UNIFORM: a wave's lanes all belong to one chunk, whose keys are then scalar loads
+
+// Puts the long run of key k, which begins in `chunk`, down for join_runs_kernel.  It ends with the last chunk that begins in it;
+// the search goes on here, where other workgroups have work to do meanwhile, by a wave at 64 chunks at a time, or by a lane.
+template <bool WAVE>
+__device__ __forceinline__ void list_run(const SumArgs& a, uint64_t chunk, uint32_t k, uint32_t lane) {
+    if (lane >= (WAVE ? 64u : 1u)) return;
+    const auto in = [&](uint64_t d) { return a.keys[(chunk + d) * a.chunk] == k; };
+    uint64_t low = 2, high = (a.count - 1u) / a.chunk - chunk + 1u;   // chunk + low - 1 begins in the run, chunk + high does not
+    if constexpr (WAVE) {
+        for (uint64_t step = 1; low < high; step = (high - low + 63u) / 64u) {   // the nearest first, which are all of most runs
+            const uint64_t probe = low + lane * step;
+            const uint32_t seen = (uint32_t)__builtin_popcountll(__builtin_amdgcn_ballot_w64(probe < high && in(probe)));
+            if (seen < 64u) high = min(high, low + seen * step);
+            if (seen > 0u) low += (seen - 1u) * step + 1u;
+        }
+    } else {
+        for (uint64_t step = 1; low < high;) {                               // twice as far each time, then half as far
+            const uint64_t probe = min(low + step - 1u, high - 1u);
+            if (in(probe)) {
+                low = probe + 1u;
+                step *= 2u;
+            } else {
+                high = probe;
+                step = (high - low + 1u) / 2u;
+            }
+        }
+    }
+    if (lane == 0u) a.joins[atomicAdd(a.join_count, 1u)] = make_uint2((uint32_t)chunk, (uint32_t)low);
+}
+
+// UNIFORM: a wave's lanes all belong to one chunk
 template <int IN, int OUT, bool UNIFORM>
 __global__ __launch_bounds__(kThreads) void sum_runs_kernel(const SumArgs a) {
-    constexpr int V = IN == kF32 ? 4 : 8;
-    const uint32_t lane = threadIdx.x & ((1u << a.shift) - 1u);
-    const uint32_t col = ((blockIdx.y << a.shift) + lane) * V;
-    if (col >= a.dim) return;
-    if (blockIdx.x >= a.chunk_blocks) {
-        uint64_t row = (uint64_t)(blockIdx.x - a.chunk_blocks) * (kThreads >> a.shift) + (threadIdx.x >> a.shift);
-        for (; row < a.out.rows; row += (uint64_t)(gridDim.x - a.chunk_blocks) * (kThreads >> a.shift)) {
-            if (a.named[row] == 0u) clear_row<OUT, V>(a.out, a.dim, row, col);
-        }
-        return;
-    }
-    uint32_t c = blockIdx.x * (kThreads >> a.shift) + (threadIdx.x >> a.shift);
-    if constexpr (UNIFORM) c = (uint32_t)__builtin_amdgcn_readfirstlane((int)c);
-    const uint64_t start = (uint64_t)c * a.chunk, end = min(start + a.chunk, a.count);
-    if (start >= a.count) return;
-    uint32_t cur = a.keys[start];
+    constexpr int V = values_of(IN, OUT);
+    __shared__ uint32_t s_key[kMostPositions + 2u * kMostChunk + 2u], s_order[kMostPositions + kMostChunk];
+    const uint32_t lane = threadIdx.x & ((1u << a.shift) - 1u), per = kThreads >> a.shift, block = blockIdx.x / a.slices;
+    const uint32_t col = (((blockIdx.x - block * a.slices) << a.shift) + lane) * V;
     const uint32_t rows = (uint32_t)a.out.rows;
-    if (cur >= rows) return;                               // keys rise: no position from here on adds to a row
-    const uint32_t last = a.keys[end - 1u];                // a run of this key may go on behind the chunk
-    bool skip = false, head = false;                       // of the run that began before this chunk
-    if (start > 0u && a.keys[start - 1u] == cur) {
-        head = continues_long(a, start, cur);
-        skip = !head;
+    const uint64_t base = (uint64_t)block * per * a.chunk;   // the workgroup's first position; s_key begins chunk + 1 before it
+    const uint32_t before = a.chunk + 1u;
+    for (uint32_t i = threadIdx.x; i < per * a.chunk + 2u * a.chunk + 2u; i += kThreads) {
+        const uint64_t p = base + i - before;                // wraps far beyond the last position
+        s_key[i] = p < a.count ? a.keys[p] : ~0u;            // no row and no token's key
     }
-    const bool tail = end < a.count && continues_long(a, end, last);   // where the last key's run goes on at all
-    const uint32_t beyond = tail ? rows : last;            // key whose positions behind the chunk belong to it: `rows` for none
+    for (uint32_t i = threadIdx.x; i < per * a.chunk + a.chunk; i += kThreads) s_order[i] = base + i < a.count ? a.order[base + i] : 0u;
+    __syncthreads();
+    uint32_t team = threadIdx.x >> a.shift;
+    if constexpr (UNIFORM) team = (uint32_t)__builtin_amdgcn_readfirstlane((int)team);
+    const auto scalar = [](uint32_t x) { return UNIFORM ? (uint32_t)__builtin_amdgcn_readfirstlane((int)x) : x; };
+    const auto key = [&](uint32_t i) { return scalar(s_key[i + before]); };   // i: from the workgroup's first position
+    // does the run of key k, which goes on across the beginning i of a chunk, reach beyond a chunk on one of its sides?
+    const auto is_long = [&](uint32_t i, uint32_t k) { return key(i - a.chunk - 1u) == k || key(i + a.chunk) == k; };
+
+    const uint32_t start = team * a.chunk, end = start + a.chunk;
+    uint32_t cur = key(start);
+    if (cur >= rows) return;                               // keys rise: no position from here on adds to a row
+    const bool continues = key(start - 1u) == cur, head = continues && is_long(start, cur);
+    const uint32_t last = key(end - 1u);
+    const bool tail = last < rows && key(end) == last && is_long(end, last);
+    const uint64_t chunk = (uint64_t)block * per + team;
+    if (tail && !(continues && cur == last) && blockIdx.x == block * a.slices) list_run<UNIFORM>(a, chunk, last, lane);
+    if (col >= a.dim) return;
+    uint32_t i = start, stop = end;
+    if (continues && !head) {                              // the chunk before this one adds it up
+        while (i < end && key(i) == cur) ++i;
+        if (i == end || key(i) >= rows) return;
+        cur = key(i);
+    }
+    if (last >= rows) {
+        while (key(stop - 1u) >= rows) --stop;
+    } else if (!tail) {
+        while (key(stop) == last) ++stop;                  // less than a chunk: the run is not long
+    }
     float sum[V] = {};
-    const auto finish = [&](bool ends) {                   // the run of `cur`, which ends here or goes on behind the chunk
-        if (head) write_partial<V>(a, c, 0u, col, sum);
-        else if (!ends && tail) write_partial<V>(a, c, 1u, col, sum);
-        else if (!skip) write_row<OUT, V>(a, cur, col, sum);
+    uint32_t run = head ? 0u : ~0u;                        // the slot of the run's partial sum; ~0u: the run is whole
+    const auto finish = [&] {
+        if (run == ~0u) {
+            write_row<OUT, V>(a, cur, col, sum);
+            return;
+        }
+        Pack<kF32, V> o;
+        o.set(sum);
+        o.store(a.partials + (2u * chunk + run) * a.width + col);   // col and width are whole numbers of V
     };
     const bool whole = col + V <= a.dim;
-    for (uint64_t i = start;; i += kRows) {
-        uint32_t key[kRows];
-        bool valid[kRows];
+    for (; i < stop; i += kRows) {
         Pack<IN, V> t[kRows];
 #pragma unroll
-        for (uint32_t j = 0; j < kRows; ++j) {
-            const bool in = i + j < a.count;
-            key[j] = in ? a.keys[i + j] : rows;
-            valid[j] = in && key[j] < rows && (i + j < end || key[j] == beyond);
+        for (uint32_t j = 0; j < kRows; ++j) {             // past the end: the last row again
+            const uint32_t from = scalar(s_order[min(i + j, stop - 1u)]);
+            const void* x = at<IN>(a.grad.data, (uint64_t)from * a.grad.stride + col);
+            if (whole) t[j].load_once(x);
+            else t[j].load_some(x, a.dim - col);
         }
 #pragma unroll
         for (uint32_t j = 0; j < kRows; ++j) {
-            if (!valid[j] || (skip && key[j] == cur)) continue;
-            const void* x = at<IN>(a.grad.data, (uint64_t)a.order[i + j] * a.grad.stride + col);
-            if (whole) {
-                t[j].load(x);
-            } else {
-                float v[V];
-#pragma unroll
-                for (int l = 0; l < V; ++l) v[l] = col + l < a.dim ? load_one<IN>(x, l) : 0.0f;
-                t[j].set(v);
-            }
-        }
-#pragma unroll
-        for (uint32_t j = 0; j < kRows; ++j) {
-            if (!valid[j]) {
-                finish(i + j < end || key[j] != last);
-                return;
-            }
-            if (key[j] != cur) {
-                finish(true);
-                cur = key[j];
-                head = skip = false;
+            if (i + j >= stop) break;
+            const uint32_t k = key(i + j);
+            if (k != cur) {
+                finish();
+                cur = k;
+                run = ~0u;
 #pragma unroll
                 for (int l = 0; l < V; ++l) sum[l] = 0.0f;
             }
-            if (!skip) {
-                float v[V];
-                t[j].get(v);
+            float v[V];
+            t[j].get(v);
 #pragma unroll
-                for (int l = 0; l < V; ++l) sum[l] += v[l];
-            }
+            for (int l = 0; l < V; ++l) sum[l] += v[l];
         }
     }
+    if (tail && run == ~0u) run = 1u;
+    finish();
 }
 
-// The partial sums of the long run that begins in a chunk: the waves take them in turn, and add up theirs in order.
-constexpr uint32_t kJoinWaves = 8, kJoinThreads = 64u * kJoinWaves;
+// The partial sums of a long run: the waves take them in turn, and add up theirs in order.
+constexpr uint32_t kJoinWaves = 8, kJoinThreads = 64u * kJoinWaves, kJoinBlocks = 256;
 template <int OUT>
 __global__ __launch_bounds__(kJoinThreads) void join_runs_kernel(const SumArgs a) {
     __shared__ float s_sum[kJoinWaves][64][4];
-    const uint64_t c = blockIdx.x, start = c * a.chunk, end = start + a.chunk;
-    if (end >= a.count) return;
-    const uint32_t k = a.keys[end];
-    if (k >= a.out.rows || a.keys[end - 1u] != k || (start > 0u && a.keys[start - 1u] == k) || !continues_long(a, end, k)) return;
     const uint32_t lane = threadIdx.x & 63u, wave = threadIdx.x >> 6, col = (blockIdx.y * 64u + lane) * 4u;
-    // chunks behind this one that begin in the run: a search by 64 at a time
-    const uint64_t most = (a.count - 1u) / a.chunk - c;
-    uint64_t low = 2, high = most + 1u;                    // chunk c + low - 1 begins in it, chunk c + high does not
-    while (low < high) {
-        const uint64_t step = (high - low + 63u) / 64u, probe = low + lane * step;
-        const bool in = probe < high && a.keys[(c + probe) * a.chunk] == k;
-        const uint32_t seen = (uint32_t)__builtin_popcountll(__builtin_amdgcn_ballot_w64(in));
-        if (seen == 0u) break;
-        const uint64_t found = low + (uint64_t)(seen - 1u) * step;   // begins in it
-        high = min(high, found + step);
-        low = found + 1u;
-    }
-    const uint64_t parts = low;                            // slot 1 of c, slot 0 of c + 1 .. c + low - 1
-    float sum[4] = {};
-    if (col < a.width) {
-        constexpr uint32_t kAhead = 4;
-        for (uint64_t p = wave; p < parts; p += kAhead * kJoinWaves) {
-            Pack<kF32, 4> t[kAhead];
+    const uint32_t joins = *a.join_count;
+    for (uint32_t n = blockIdx.x; n < joins; n += gridDim.x) {
+        const uint2 join = a.joins[n];
+        const uint64_t c = join.x, parts = join.y;                    // slot 1 of c, slot 0 of c + 1 .. c + parts - 1
+        const uint32_t k = a.keys[(c + 1u) * a.chunk];
+        float sum[4] = {};
+        if (col < a.width) {
+            constexpr uint32_t kAhead = 8;
+            for (uint64_t p = wave; p < parts; p += kAhead * kJoinWaves) {
+                Pack<kF32, 4> t[kAhead];
 #pragma unroll
-            for (uint32_t j = 0; j < kAhead; ++j) {
-                const uint64_t q = p + j * kJoinWaves;
-                if (q < parts) t[j].load(a.partials + (2u * (c + q) + (q == 0u ? 1u : 0u)) * a.width + col);
-            }
+                for (uint32_t j = 0; j < kAhead; ++j) {
+                    const uint64_t part = min(p + j * kJoinWaves, parts - 1u);
+                    t[j].load(a.partials + (2u * (c + part) + (part == 0u ? 1u : 0u)) * a.width + col);
+                }
 #pragma unroll
-            for (uint32_t j = 0; j < kAhead; ++j) {
-                if (p + j * kJoinWaves >= parts) continue;
-                float v[4];
-                t[j].get(v);
+                for (uint32_t j = 0; j < kAhead; ++j) {
+                    if (p + j * kJoinWaves >= parts) break;
+                    float v[4];
+                    t[j].get(v);
 #pragma unroll
-                for (int l = 0; l < 4; ++l) sum[l] += v[l];
+                    for (int l = 0; l < 4; ++l) sum[l] += v[l];
+                }
             }
         }
+        __syncthreads();                                              // the run before this one has been added up
+#pragma unroll
+        for (int l = 0; l < 4; ++l) s_sum[wave][lane][l] = sum[l];
+        __syncthreads();
+        if (wave == 0u && col < a.dim) {
+#pragma unroll
+            for (uint32_t w = 1; w < kJoinWaves; ++w) {
+#pragma unroll
+                for (int l = 0; l < 4; ++l) sum[l] += s_sum[w][lane][l];
+            }
+            write_row<OUT, 4>(a, k, col, sum);
+        }
     }
-#pragma unroll
-    for (int l = 0; l < 4; ++l) s_sum[wave][lane][l] = sum[l];
-    __syncthreads();
-    if (wave != 0u || col >= a.dim) return;
-#pragma unroll
-    for (uint32_t w = 1; w < kJoinWaves; ++w) {
-#pragma unroll
-        for (int l = 0; l < 4; ++l) sum[l] += s_sum[w][lane][l];
-    }
-    write_row<OUT, 4>(a, k, col, sum);
 }
 
-// lanes that hold a row, as a power of two of at most a workgroup, and slices of a row
-uint32_t row_shift(uint32_t dim, uint32_t v) {
-    uint32_t shift = 0;
-    while ((1u << shift) < kThreads && (1u << shift) * v < dim) ++shift;
-    return shift;
-}
-constexpr uint64_t kMaxBlocks = 1u << 22;   // a launch holds less than 2^32 lanes: the workgroups take rows in turn from there on
-dim3 row_grid(uint64_t rows, uint32_t dim, uint32_t v) {
-    const uint32_t shift = row_shift(dim, v), per = kThreads >> shift, width = v << shift;
-    return dim3((uint32_t)std::min<uint64_t>((rows + per - 1u) / per, kMaxBlocks), (dim + width - 1u) / width);
+// How `rows` rows are shared out: 1 << shift lanes hold a row, or one of `slices` slices of it; the workgroups take rows in turn
+// where a launch, which holds less than 2^32 lanes, has no workgroup for each.
+struct RowShape {
+    uint32_t shift, slices, blocks;
+};
+constexpr uint64_t kMaxBlocks = 1u << 23;
+RowShape row_shape(uint64_t rows, uint32_t dim, uint32_t v) {
+    RowShape s = {};
+    while ((1u << s.shift) < kThreads && (1u << s.shift) * v < dim) ++s.shift;
+    s.slices = (dim + (v << s.shift) - 1u) / (v << s.shift);
+    const uint64_t per = kThreads >> s.shift, most = std::max<uint64_t>(1, kMaxBlocks / s.slices);
+    s.blocks = (uint32_t)std::min<uint64_t>((rows + per - 1u) / per, most) * s.slices;
+    return s;
 }
 
-// Positions of a chunk: enough chunks to fill the GPU, as long as that allows (a long run leaves a partial sum in every chunk).
+// Positions of a chunk: enough chunks to fill the GPU, as long as that allows (a long run leaves a partial sum in every chunk),
+// and no more than LDS holds of a workgroup's.  The same for all types, which the size of the workspace does not depend on.
 uint32_t chunk_of(uint64_t tokens, uint32_t dim) {
+    const uint32_t per = kThreads >> row_shape(1, dim, 8u).shift;   // most chunks of a workgroup: 8 values a lane
     const uint64_t waves = tokens * ((dim + 511u) / 512u);
-    uint32_t chunk = 8;
-    while (chunk < 64u && waves / (2u * chunk) >= 4096u) chunk *= 2u;
-    while (tokens / chunk >= kMaxBlocks) chunk *= 2u;
+    uint32_t chunk = kMostPositions / kThreads;
+    while (chunk < kMostChunk && per * chunk < kMostPositions && waves / (2u * chunk) >= 4096u) chunk *= 2u;
     return chunk;
 }
 
 struct GradWorkspace {
-    uint32_t *keys[2], *order[2], *counts, *named;
+    uint32_t *keys[2], *order[2], *counts, *named, *join_count;
+    uint2* joins;
     float* partials;
     size_t bytes;
 };
@@ -469,8 +564,10 @@ GradWorkspace grad_workspace(void* base, uint64_t tokens, uint32_t dim, uint64_t
         w.order[i] = take(tokens);
     }
     w.counts = take((uint64_t)s.ranges << s.bits);
-    const uint32_t chunk = chunk_of(tokens, dim);
-    w.partials = reinterpret_cast<float*>(take((tokens + chunk - 1u) / chunk * 2u * ((dim + 7u) & ~7u)));
+    const uint64_t chunks = (tokens + chunk_of(tokens, dim) - 1u) / chunk_of(tokens, dim);
+    w.join_count = take(1);
+    w.joins = reinterpret_cast<uint2*>(take(chunks + 2u));        // of two neighbours, one at most: a long run covers the chunk behind the one it begins in
+    w.partials = reinterpret_cast<float*>(take(chunks * 2u * ((dim + 7u) & ~7u)));
     return w;
 }
 
@@ -480,11 +577,10 @@ hipError_t launch_embedding(const RowMatrix& table, const TokenIds& ids, uint32_
     if (ids.count == 0) return hipSuccess;
     with_dtype(table.dtype, [&](auto in) {
         with_dtype(out.dtype, [&](auto o) {
-            constexpr uint32_t v = in == kF32 || o == kF32 ? 4u : 8u;
-            const dim3 grid = row_grid(ids.count, dim, v);
-            const uint32_t shift = row_shift(dim, v);
-            if (ids.wide) hipLaunchKernelGGL((embedding_kernel<in, o, true>), grid, dim3(kThreads), 0, stream, table, ids, dim, shift, scale, out);
-            else hipLaunchKernelGGL((embedding_kernel<in, o, false>), grid, dim3(kThreads), 0, stream, table, ids, dim, shift, scale, out);
+            constexpr uint32_t v = values_of(in, o);
+            const RowShape g = row_shape((ids.count + kLookups - 1u) / kLookups, dim, v);
+            hipLaunchKernelGGL((ids.wide ? embedding_kernel<in, o, true> : embedding_kernel<in, o, false>), dim3(g.blocks), dim3(kThreads), 0, stream, table, ids,
+                               dim, g.shift, g.slices, scale, out);
         });
     });
     return hipGetLastError();
@@ -494,21 +590,16 @@ size_t embedding_grad_workspace(uint64_t tokens, uint32_t dim, uint64_t rows) { 
 
 hipError_t launch_embedding_grad(const RowMatrix& grad_out, const TokenIds& ids, uint32_t dim, float scale, const RowMatrix& table_grad,
                                  bool accumulate, void* workspace, hipStream_t stream) {
-    SumArgs b = {};
-    b.count = ids.count;
-    b.grad = grad_out;
-    b.out = table_grad;
-    b.dim = dim;
-    b.width = (dim + 7u) & ~7u;
-    b.scale = scale;
-    b.accumulate = accumulate;
-    hipError_t e = hipSuccess;
+    ClearRows clear = {};
+    clear.out = table_grad;
+    clear.dim = dim;
+    const auto clear_shape = [&](uint64_t rows) { return row_shape(rows, dim, table_grad.dtype == kF32 ? 4u : 8u); };
+    clear.shift = clear_shape(1).shift;
+    clear.slices = clear_shape(1).slices;
     if (ids.count == 0) {
-        if (accumulate) return e;
-        with_dtype(table_grad.dtype, [&](auto o) {
-            constexpr uint32_t v = o == kF32 ? 4u : 8u;
-            hipLaunchKernelGGL((clear_rows_kernel<o>), row_grid(table_grad.rows, dim, v), dim3(kThreads), 0, stream, table_grad, dim, row_shift(dim, v));
-        });
+        if (accumulate) return hipSuccess;
+        clear.end = table_grad.rows;
+        hipLaunchKernelGGL(clear_rows_kernel, dim3(clear_shape(clear.end).blocks / clear.slices), dim3(kThreads), 0, stream, clear);
         return hipGetLastError();
     }
     const GradWorkspace w = grad_workspace(workspace, ids.count, dim, table_grad.rows);
@@ -521,40 +612,63 @@ hipError_t launch_embedding_grad(const RowMatrix& grad_out, const TokenIds& ids,
     a.ranges = s.ranges;
     a.bits = s.bits;
     a.named = accumulate ? nullptr : reinterpret_cast<uint4*>(w.named);
+    a.join_count = w.join_count;
+    // The rows to clear are shared out over the launches of the sort: to each but the last as much as takes about as long as the
+    // launch does without, to the last all that is left.  Rows that are cleared before the names are known are cleared for
+    // nothing where they are named, which the last rows of a vocabulary seldom are: from the last row on.
+    uint64_t left = accumulate ? 0 : table_grad.rows;
+    const uint64_t beside = std::max<uint64_t>(1, kClearBeside / ((uint64_t)dim * bytes_of(table_grad.dtype)));
+    const auto share = [&](bool rest) {
+        clear.end = left;
+        left -= rest ? left : std::min(left, beside);
+        clear.first = left;
+        return (uint32_t)std::min<uint64_t>(kClearBlocks, clear.end - clear.first);
+    };
+    hipError_t e;
     for (uint32_t pass = 0; pass < s.passes; ++pass) {
         a.keys_out = w.keys[pass & 1u];
         a.order_out = w.order[pass & 1u];
         a.shift = pass * s.bits;
-        const uint64_t clearing = a.named == nullptr ? 0 : a.rows / (64u * kSortThreads);   // four 16-byte stores a lane
-        const uint32_t count_blocks = (uint32_t)std::max<uint64_t>(s.ranges, std::min<uint64_t>(clearing, 2048));
-        hipLaunchKernelGGL((ids.wide ? sort_count_kernel<true> : sort_count_kernel<false>), dim3(count_blocks), dim3(kSortThreads), 0, stream, a);
-        hipLaunchKernelGGL((ids.wide ? sort_scatter_kernel<true> : sort_scatter_kernel<false>), dim3(s.ranges), dim3(kSortThreads), 0, stream, a);
+        clear.named = pass == 0u ? nullptr : reinterpret_cast<const uint8_t*>(w.named);
+        uint32_t more = share(false);
+        if (a.named != nullptr) more = std::max<uint32_t>(more, (uint32_t)std::min<uint64_t>(kClearBlocks, a.rows / (32u * kSortThreads)));
+        hipLaunchKernelGGL((ids.wide ? sort_count_kernel<true> : sort_count_kernel<false>), dim3(s.ranges + more), dim3(kSortThreads), 0, stream, a, clear);
+        more = share(pass + 1u == s.passes);
+        hipLaunchKernelGGL((ids.wide ? sort_scatter_kernel<true> : sort_scatter_kernel<false>), dim3(s.ranges + more), dim3(kSortThreads), 0, stream, a, clear);
         e = hipGetLastError();
         if (e != hipSuccess) return e;
         a.keys = a.keys_out;
         a.order = a.order_out;
         a.named = nullptr;
     }
+    SumArgs b = {};
     b.keys = a.keys;
     b.order = a.order;
+    b.count = ids.count;
+    b.grad = grad_out;
+    b.out = table_grad;
     b.partials = w.partials;
-    b.named = accumulate ? nullptr : reinterpret_cast<const uint8_t*>(w.named);
+    b.joins = w.joins;
+    b.join_count = w.join_count;
+    b.dim = dim;
+    b.width = (dim + 7u) & ~7u;
     b.chunk = chunk_of(ids.count, dim);
+    b.scale = scale;
+    b.accumulate = accumulate;
     const uint64_t chunks = (ids.count + b.chunk - 1u) / b.chunk;
     with_dtype(grad_out.dtype, [&](auto in) {
         with_dtype(table_grad.dtype, [&](auto o) {
-            constexpr uint32_t v = in == kF32 ? 4u : 8u;
-            b.shift = row_shift(dim, v);
-            dim3 grid = row_grid(chunks, dim, v);
-            b.chunk_blocks = grid.x;
-            if (!accumulate) grid.x += row_grid(b.out.rows, dim, v).x;
-            hipLaunchKernelGGL((b.shift >= 6u ? sum_runs_kernel<in, o, true> : sum_runs_kernel<in, o, false>), grid, dim3(kThreads), 0, stream, b);
+            constexpr uint32_t v = values_of(in, o);
+            const RowShape g = row_shape(chunks, dim, v);
+            b.shift = g.shift;
+            b.slices = g.slices;
+            hipLaunchKernelGGL((b.shift >= 6u ? sum_runs_kernel<in, o, true> : sum_runs_kernel<in, o, false>), dim3(g.blocks), dim3(kThreads), 0, stream, b);
         });
     });
     e = hipGetLastError();
     if (e != hipSuccess || chunks < 3u) return e;   // a long run touches three chunks
     with_dtype(table_grad.dtype, [&](auto o) {
-        hipLaunchKernelGGL((join_runs_kernel<o>), dim3((uint32_t)chunks, (b.width + 255u) / 256u), dim3(kJoinThreads), 0, stream, b);
+        hipLaunchKernelGGL((join_runs_kernel<o>), dim3((uint32_t)std::min<uint64_t>(chunks / 2u, kJoinBlocks), (b.width + 255u) / 256u), dim3(kJoinThreads), 0, stream, b);
     });
     return hipGetLastError();
 }

@@ -12,6 +12,19 @@ namespace values {
 constexpr int kF32 = MQG_FLOAT32, kF16 = MQG_FLOAT16, kBF16 = MQG_BFLOAT16;
 constexpr uint32_t bytes_of(int dtype) { return dtype == kF32 ? 4u : 2u; }
 
+// one value
+template <int DTYPE>
+__device__ __forceinline__ float load_one(const void* p, uint64_t i) {
+    if constexpr (DTYPE == kF32) return reinterpret_cast<const float*>(p)[i];
+    else if constexpr (DTYPE == kF16) return (float)reinterpret_cast<const _Float16*>(p)[i];
+    else return __builtin_bit_cast(float, (uint32_t)reinterpret_cast<const uint16_t*>(p)[i] << 16);
+}
+template <int DTYPE>
+__device__ __forceinline__ void store_one(void* p, uint64_t i, float x) {
+    if constexpr (DTYPE == kF32) reinterpret_cast<float*>(p)[i] = x;
+    else if constexpr (DTYPE == kF16) reinterpret_cast<_Float16*>(p)[i] = (_Float16)x;
+    else reinterpret_cast<__bf16*>(p)[i] = (__bf16)x;
+}
 template <int BYTES>
 struct Words;
 template <>
@@ -61,6 +74,13 @@ struct Pack {
             }
         }
     }
+    // the first `count` of V values, the others 0
+    __device__ __forceinline__ void load_some(const void* p, uint32_t count) {
+        float x[V];
+#pragma unroll
+        for (int i = 0; i < V; ++i) x[i] = (uint32_t)i < count ? load_one<DTYPE>(p, i) : 0.0f;
+        set(x);
+    }
     // rounded once, to the nearest value, ties to even
     __device__ __forceinline__ void set(const float (&x)[V]) {
         uint32_t w[kBytes / 4];
@@ -78,19 +98,6 @@ struct Pack {
     }
 };
 
-// one value
-template <int DTYPE>
-__device__ __forceinline__ float load_one(const void* p, uint64_t i) {
-    if constexpr (DTYPE == kF32) return reinterpret_cast<const float*>(p)[i];
-    else if constexpr (DTYPE == kF16) return (float)reinterpret_cast<const _Float16*>(p)[i];
-    else return __builtin_bit_cast(float, (uint32_t)reinterpret_cast<const uint16_t*>(p)[i] << 16);
-}
-template <int DTYPE>
-__device__ __forceinline__ void store_one(void* p, uint64_t i, float x) {
-    if constexpr (DTYPE == kF32) reinterpret_cast<float*>(p)[i] = x;
-    else if constexpr (DTYPE == kF16) reinterpret_cast<_Float16*>(p)[i] = (_Float16)x;
-    else reinterpret_cast<__bf16*>(p)[i] = (__bf16)x;
-}
 template <int DTYPE>
 __device__ __forceinline__ const void* at(const void* p, uint64_t i) { return static_cast<const char*>(p) + i * bytes_of(DTYPE); }
 template <int DTYPE>
