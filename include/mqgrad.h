@@ -464,7 +464,7 @@ typedef enum { MQG_INDEX32 = 0, MQG_INDEX64 = 1 } mqg_index_type;
 
 #define MQG_MAX_TOKENS 0x7FFFFFFFu
 #define MQG_MAX_TABLE_ROWS 0x7FFFFFFFu
-#define MQG_MAX_ROW_DIM 0x1000000u
+#define MQG_MAX_ROW_DIM 0x100000u
 
 typedef struct {
     void* data;       /* device, aligned to one value; values [r * stride, r * stride + dim) are row r.  Written only where the call says so. */

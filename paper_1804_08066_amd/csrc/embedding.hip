@@ -164,6 +164,25 @@ __device__ __forceinline__ uint32_t sort_key(const SortArgs& a, uint64_t i) {
     return a.keys != nullptr ? a.keys[i] : row_of<WIDE>(a.ids, i, a.rows, true);
 }
 
+// How many keys of digit d come before this lane's: those that counts[d] holds from before, and those of lower lanes.  Adds the wave's
+// keys to `counts`, which is the wave's own.
+template <class Count>
+__device__ __forceinline__ uint32_t rank_in_wave(Count* counts, uint32_t d, uint32_t bits, bool valid) {
+    uint64_t same = __builtin_amdgcn_ballot_w64(valid);
+    for (uint32_t b = 0; b < bits; ++b) {
+        const bool one = (d >> b) & 1u;
+        const uint64_t ones = __builtin_amdgcn_ballot_w64(one);
+        same &= one ? ones : ~ones;
+    }
+    const uint32_t below = __builtin_amdgcn_mbcnt_hi((uint32_t)(same >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)same, 0u));
+    uint32_t seen = 0;
+    if (valid) seen = __hip_atomic_load(&counts[d], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WAVEFRONT);
+    __builtin_amdgcn_wave_barrier();   // a wave's LDS operations keep their order: all have read before one writes
+    if (valid && below == 0u) __hip_atomic_store(&counts[d], (Count)(seen + (uint32_t)__builtin_popcountll(same)), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WAVEFRONT);
+    __builtin_amdgcn_wave_barrier();
+    return seen + below;
+}
+
 template <bool WIDE>
 __global__ __launch_bounds__(kSortThreads) void sort_count_kernel(const SortArgs a, const ClearRows c) {
     __shared__ uint32_t s_count[kMaxDigits];
@@ -271,22 +290,7 @@ __global__ __launch_bounds__(kSortThreads) void sort_scatter_kernel(const SortAr
         __builtin_amdgcn_wave_barrier();
 #pragma unroll
         for (uint32_t j = 0; j < kSortItems; ++j) {
-            const uint32_t d = (key[j] >> a.shift) & (digits - 1u);
-            uint64_t same = __builtin_amdgcn_ballot_w64(valid[j]);
-            for (uint32_t b = 0; b < a.bits; ++b) {
-                const bool one = (d >> b) & 1u;
-                const uint64_t ones = __builtin_amdgcn_ballot_w64(one);
-                same &= one ? ones : ~ones;
-            }
-            const uint32_t below = __builtin_amdgcn_mbcnt_hi((uint32_t)(same >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)same, 0u));
-            uint32_t seen = 0;
-            if (valid[j]) seen = __hip_atomic_load(&s_wave[wave][d], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WAVEFRONT);
-            __builtin_amdgcn_wave_barrier();   // a wave's LDS operations keep their order: all have read before one writes
-            if (valid[j] && below == 0u) {
-                __hip_atomic_store(&s_wave[wave][d], seen + (uint32_t)__builtin_popcountll(same), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WAVEFRONT);
-            }
-            __builtin_amdgcn_wave_barrier();
-            rank[j] = seen + below;
+            rank[j] = rank_in_wave(s_wave[wave], (key[j] >> a.shift) & (digits - 1u), a.bits, valid[j]);
         }
         __syncthreads();
         for (uint32_t d = tid; d < digits; d += kSortThreads) {
@@ -309,6 +313,196 @@ __global__ __launch_bounds__(kSortThreads) void sort_scatter_kernel(const SortAr
             if (a.named != nullptr && key[j] < a.rows) reinterpret_cast<uint8_t*>(a.named)[key[j]] = 1u;
         }
     }
+}
+
+// The same in one workgroup, for batches that it holds: the digits' counts, the scatters and the keys between them stay in LDS.
+// A launch of the passes above mostly waits for memory and for the launch before it: the gradient of 4096 positions of 1024 values
+// took 37 us with them and takes 27, of which the sort 12; of 8192 positions 41 and 39; of 16384, in a workgroup that holds them, 66
+// instead of 51.
+constexpr uint32_t kOneThreads = 1024, kOneWaves = kOneThreads / 64u, kOneItems = 8, kOneTokens = kOneThreads * kOneItems;
+template <bool WIDE>
+__global__ __launch_bounds__(kOneThreads) void sort_one_kernel(const SortArgs a, const ClearRows c, const uint32_t passes) {
+    __shared__ uint32_t s_key[kOneTokens];
+    __shared__ uint16_t s_order[kOneTokens], s_wave[kOneWaves][kMaxDigits];
+    __shared__ uint32_t s_total[kOneWaves];
+    if (blockIdx.x > 0u) {
+        clear_rows(c, blockIdx.x - 1u, gridDim.x - 1u);
+        return;
+    }
+    const uint32_t digits = 1u << a.bits, tid = threadIdx.x, lane = tid & 63u, wave = tid >> 6, count = (uint32_t)a.ids.count;
+    const uint32_t items = (count + kOneThreads - 1u) / kOneThreads, first = wave * 64u * items + lane;   // a wave's keys are consecutive
+    if (tid == 0u) *a.join_count = 0u;
+    uint32_t key[kOneItems], from[kOneItems], rank[kOneItems];
+#pragma unroll
+    for (uint32_t j = 0; j < kOneItems; ++j) {
+        from[j] = first + j * 64u;
+        key[j] = j < items && from[j] < count ? row_of<WIDE>(a.ids, from[j], a.rows, true) : 0u;
+    }
+    for (uint32_t pass = 0; pass < passes; ++pass) {
+        const uint32_t shift = pass * a.bits;
+        for (uint32_t d = lane; d < digits; d += 64u) s_wave[wave][d] = 0u;
+        __builtin_amdgcn_wave_barrier();
+#pragma unroll
+        for (uint32_t j = 0; j < kOneItems; ++j) {
+            if (j >= items) break;
+            const uint32_t d = (key[j] >> shift) & (digits - 1u);
+            const bool valid = first + j * 64u < count;
+            rank[j] = rank_in_wave(s_wave[wave], d, a.bits, valid);
+        }
+        __syncthreads();
+        uint32_t all = 0;   // of digit tid
+        if (tid < digits) {
+#pragma unroll
+            for (uint32_t w = 0; w < kOneWaves; ++w) {
+                const uint32_t n = s_wave[w][tid];
+                s_wave[w][tid] = (uint16_t)all;
+                all += n;
+            }
+        }
+        uint32_t upto = all;
+#pragma unroll
+        for (uint32_t m = 1; m < 64u; m <<= 1) {
+            const uint32_t other = __shfl_up(upto, m, 64);
+            if (lane >= m) upto += other;
+        }
+        if (lane == 63u) s_total[wave] = upto;
+        __syncthreads();
+        uint32_t before = upto - all;
+        for (uint32_t w = 0; w < wave; ++w) before += s_total[w];
+        if (tid < digits) {
+#pragma unroll
+            for (uint32_t w = 0; w < kOneWaves; ++w) s_wave[w][tid] = (uint16_t)(s_wave[w][tid] + before);
+        }
+        __syncthreads();
+#pragma unroll
+        for (uint32_t j = 0; j < kOneItems; ++j) {
+            if (j >= items) break;
+            if (first + j * 64u >= count) continue;
+            const uint32_t to = s_wave[wave][(key[j] >> shift) & (digits - 1u)] + rank[j];
+            s_key[to] = key[j];
+            s_order[to] = (uint16_t)from[j];
+        }
+        __syncthreads();
+#pragma unroll
+        for (uint32_t j = 0; j < kOneItems; ++j) {
+            const uint32_t i = first + j * 64u;
+            if (j >= items) break;
+            if (i >= count) continue;
+            key[j] = s_key[i];
+            from[j] = s_order[i];
+            if (pass + 1u == passes) {
+                a.keys_out[i] = key[j];
+                a.order_out[i] = from[j];
+            }
+        }
+    }
+}
+
+// ---- a few positions ------------------------------------------------------------------------------------
+// Without a sort: every workgroup finds the positions of its position's row among all of them, and adds up their slice of
+// grad_out where its own is the first.  One launch of 5 us for 500 positions of 512 values, where sort, sums and joins take 16; 512
+// positions of 4096 values take 16.3 and 17.6, 1000 take 41 and 20.
+constexpr uint32_t kFewTokens = 512, kFewSum = 8, kFewRows = 1024;
+struct FewArgs {
+    TokenIds ids;
+    RowMatrix grad, out;
+    uint32_t dim, slices;    // a wave holds a slice of a row
+    uint32_t sums;           // workgroups that add up; the others clear clear_rows rows each
+    uint32_t clear_rows, clear_shift, clear_slices;
+    float scale;
+    bool accumulate;
+};
+template <int IN, int OUT, bool WIDE>
+__global__ __launch_bounds__(kThreads) void sum_few_kernel(const FewArgs a) {
+    constexpr int V = values_of(IN, OUT);
+    constexpr uint32_t kWaves = kThreads / 64u;
+    __shared__ uint32_t s_key[kFewTokens], s_list[kFewTokens];
+    __shared__ float s_sum[kWaves - 1u][64][V];
+    __shared__ uint8_t s_named[kFewRows];
+    const uint32_t count = (uint32_t)a.ids.count, rows = (uint32_t)a.out.rows, tid = threadIdx.x, lane = tid & 63u;
+    const uint32_t wave = (uint32_t)__builtin_amdgcn_readfirstlane((int)(tid >> 6));
+    for (uint32_t i = tid; i < count; i += kThreads) s_key[i] = row_of<WIDE>(a.ids, i, rows, true);
+    if (blockIdx.x >= a.sums) {
+        constexpr int VC = OUT == kF32 ? 4 : 8;
+        const uint64_t first = (uint64_t)(blockIdx.x - a.sums) * a.clear_rows, end = min(first + a.clear_rows, a.out.rows);
+        for (uint32_t i = tid; i < a.clear_rows; i += kThreads) s_named[i] = 0u;
+        __syncthreads();
+        for (uint32_t i = tid; i < count; i += kThreads) {
+            if (s_key[i] >= first && s_key[i] < end) s_named[s_key[i] - first] = 1u;
+        }
+        __syncthreads();
+        const float zero[VC] = {};
+        for (uint64_t row = first + (tid >> a.clear_shift); row < end; row += kThreads >> a.clear_shift) {
+            if (s_named[row - first] != 0u) continue;
+            for (uint32_t s = 0; s < a.clear_slices; ++s) {
+                const uint32_t col = ((s << a.clear_shift) + (tid & ((1u << a.clear_shift) - 1u))) * VC;
+                if (col < a.dim) store_values<OUT>(at<OUT>(a.out.data, row * a.out.stride + col), zero, a.dim - col, true);
+            }
+        }
+        return;
+    }
+    __syncthreads();
+    const uint32_t p = blockIdx.x / a.slices, col = ((blockIdx.x - p * a.slices) * 64u + lane) * V;
+    const uint32_t k = s_key[p];
+    if (k >= rows) return;
+    const bool in = col < a.dim, whole = col + V <= a.dim;
+    Pack<OUT, V> old;
+    void* y = at<OUT>(a.out.data, (uint64_t)k * a.out.stride + col);
+    uint32_t found = 0;
+    for (uint32_t i = 0; i < count; i += 64u) {
+        const bool mine = i + lane < count && s_key[i + lane] == k;
+        const uint64_t all = __builtin_amdgcn_ballot_w64(mine);
+        if (found == 0u && all != 0u && i + (uint32_t)__builtin_ctzll(all) < p) return;   // an earlier position's workgroup adds the row up
+        const uint32_t below = __builtin_amdgcn_mbcnt_hi((uint32_t)(all >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)all, 0u));
+        if (mine && wave == 0u) s_list[found + below] = i + lane;
+        found += (uint32_t)__builtin_popcountll(all);
+    }
+    if (a.accumulate && wave == 0u && in) {
+        if (whole) old.load(y);
+        else old.load_some(y, a.dim - col);
+    }
+    __syncthreads();
+    float sum[V] = {};
+    for (uint32_t n = wave; n < found; n += kWaves * kFewSum) {   // the waves take the positions in turn
+        Pack<IN, V> t[kFewSum];
+#pragma unroll
+        for (uint32_t j = 0; j < kFewSum; ++j) {
+            if (!in || n + j * kWaves >= found) break;
+            const void* x = at<IN>(a.grad.data, (uint64_t)s_list[n + j * kWaves] * a.grad.stride + col);
+            if (whole) t[j].load(x);
+            else t[j].load_some(x, a.dim - col);
+        }
+#pragma unroll
+        for (uint32_t j = 0; j < kFewSum; ++j) {
+            if (!in || n + j * kWaves >= found) break;
+            float v[V];
+            t[j].get(v);
+#pragma unroll
+            for (int l = 0; l < V; ++l) sum[l] += v[l];
+        }
+    }
+    if (found > 1u) {
+        if (wave > 0u) {
+#pragma unroll
+            for (int l = 0; l < V; ++l) s_sum[wave - 1u][lane][l] = sum[l];
+        }
+        __syncthreads();
+    }
+    if (wave > 0u || !in) return;
+    for (uint32_t w = 1; w < min(found, kWaves); ++w) {
+#pragma unroll
+        for (int l = 0; l < V; ++l) sum[l] += s_sum[w - 1u][lane][l];
+    }
+    float v[V];
+    if (a.accumulate) {
+        old.get(v);
+#pragma unroll
+        for (int l = 0; l < V; ++l) v[l] = __builtin_fmaf(a.scale, sum[l], v[l]);
+    } else {
+#pragma unroll
+        for (int l = 0; l < V; ++l) v[l] = a.scale * sum[l];
+    }
+    store_values<OUT>(y, v, a.dim - col, !a.accumulate);
 }
 
 // ---- the sums ------------------------------------------------------------------------------------------
@@ -385,15 +579,13 @@ __device__ __forceinline__ void list_run(const SumArgs& a, uint64_t chunk, uint3
     if (lane == 0u) a.joins[atomicAdd(a.join_count, 1u)] = make_uint2((uint32_t)chunk, (uint32_t)low);
 }
 
-// UNIFORM: a wave's lanes all belong to one chunk
+// The chunks of a workgroup, in one slice.  UNIFORM: a wave's lanes all belong to one chunk.
 template <int IN, int OUT, bool UNIFORM>
-__global__ __launch_bounds__(kThreads) void sum_runs_kernel(const SumArgs a) {
+__device__ __forceinline__ void sum_chunks(const SumArgs& a, const uint64_t block, const uint32_t slice, uint32_t* s_key, uint32_t* s_order) {
     constexpr int V = values_of(IN, OUT);
-    __shared__ uint32_t s_key[kMostPositions + 2u * kMostChunk + 2u], s_order[kMostPositions + kMostChunk];
-    const uint32_t lane = threadIdx.x & ((1u << a.shift) - 1u), per = kThreads >> a.shift, block = blockIdx.x / a.slices;
-    const uint32_t col = (((blockIdx.x - block * a.slices) << a.shift) + lane) * V;
+    const uint32_t lane = threadIdx.x & ((1u << a.shift) - 1u), per = kThreads >> a.shift, col = ((slice << a.shift) + lane) * V;
     const uint32_t rows = (uint32_t)a.out.rows;
-    const uint64_t base = (uint64_t)block * per * a.chunk;   // the workgroup's first position; s_key begins chunk + 1 before it
+    const uint64_t base = block * per * a.chunk;             // the workgroup's first position; s_key begins chunk + 1 before it
     const uint32_t before = a.chunk + 1u;
     for (uint32_t i = threadIdx.x; i < per * a.chunk + 2u * a.chunk + 2u; i += kThreads) {
         const uint64_t p = base + i - before;                // wraps far beyond the last position
@@ -414,8 +606,8 @@ __global__ __launch_bounds__(kThreads) void sum_runs_kernel(const SumArgs a) {
     const bool continues = key(start - 1u) == cur, head = continues && is_long(start, cur);
     const uint32_t last = key(end - 1u);
     const bool tail = last < rows && key(end) == last && is_long(end, last);
-    const uint64_t chunk = (uint64_t)block * per + team;
-    if (tail && !(continues && cur == last) && blockIdx.x == block * a.slices) list_run<UNIFORM>(a, chunk, last, lane);
+    const uint64_t chunk = block * per + team;
+    if (tail && !(continues && cur == last) && slice == 0u) list_run<UNIFORM>(a, chunk, last, lane);
     if (col >= a.dim) return;
     uint32_t i = start, stop = end;
     if (continues && !head) {                              // the chunk before this one adds it up
@@ -468,6 +660,16 @@ __global__ __launch_bounds__(kThreads) void sum_runs_kernel(const SumArgs a) {
     }
     if (tail && run == ~0u) run = 1u;
     finish();
+}
+template <int IN, int OUT, bool UNIFORM>
+__global__ __launch_bounds__(kThreads) void sum_runs_kernel(const SumArgs a) {
+    __shared__ uint32_t s_key[kMostPositions + 2u * kMostChunk + 2u], s_order[kMostPositions + kMostChunk];
+    const uint32_t first = blockIdx.x / a.slices, slice = blockIdx.x - first * a.slices;
+    const uint64_t blocks = (a.count + (uint64_t)(kThreads >> a.shift) * a.chunk - 1u) / ((kThreads >> a.shift) * a.chunk);
+    for (uint64_t block = first; block < blocks; block += gridDim.x / a.slices) {
+        sum_chunks<IN, OUT, UNIFORM>(a, block, slice, s_key, s_order);
+        __syncthreads();
+    }
 }
 
 // The partial sums of a long run: the waves take them in turn, and add up theirs in order.
@@ -549,9 +751,9 @@ struct GradWorkspace {
 };
 GradWorkspace grad_workspace(void* base, uint64_t tokens, uint32_t dim, uint64_t rows) {
     GradWorkspace w = {};
+    if (tokens <= kFewTokens) return w;
     w.named = static_cast<uint32_t*>(base);
-    w.bytes = (rows + 15u) & ~(uint64_t)15u;
-    if (tokens == 0) return w;
+    if (tokens > kOneTokens) w.bytes = (rows + 15u) & ~(uint64_t)15u;
     const SortShape s = sort_shape(tokens, rows);
     char* p = static_cast<char*>(base);
     const auto take = [&](uint64_t words) {
@@ -602,6 +804,30 @@ hipError_t launch_embedding_grad(const RowMatrix& grad_out, const TokenIds& ids,
         hipLaunchKernelGGL(clear_rows_kernel, dim3(clear_shape(clear.end).blocks / clear.slices), dim3(kThreads), 0, stream, clear);
         return hipGetLastError();
     }
+    if (ids.count <= kFewTokens) {
+        FewArgs f = {};
+        f.ids = ids;
+        f.grad = grad_out;
+        f.out = table_grad;
+        f.dim = dim;
+        f.scale = scale;
+        f.accumulate = accumulate;
+        f.clear_shift = clear.shift;
+        f.clear_slices = clear.slices;
+        // a workgroup clears 16 KB at least; 4096 workgroups, or as many as hold the rows
+        const uint64_t row_bytes = (uint64_t)dim * bytes_of(table_grad.dtype);
+        f.clear_rows = (uint32_t)std::min<uint64_t>(kFewRows, std::max<uint64_t>({1u, 16384u / row_bytes, (table_grad.rows + 4095u) / 4096u}));
+        const uint32_t clears = accumulate ? 0u : (uint32_t)((table_grad.rows + f.clear_rows - 1u) / f.clear_rows);
+        with_dtype(grad_out.dtype, [&](auto in) {
+            with_dtype(table_grad.dtype, [&](auto o) {
+                constexpr uint32_t width = 64u * values_of(in, o);
+                f.slices = (dim + width - 1u) / width;
+                f.sums = (uint32_t)ids.count * f.slices;
+                hipLaunchKernelGGL((ids.wide ? sum_few_kernel<in, o, true> : sum_few_kernel<in, o, false>), dim3(f.sums + clears), dim3(kThreads), 0, stream, f);
+            });
+        });
+        return hipGetLastError();
+    }
     const GradWorkspace w = grad_workspace(workspace, ids.count, dim, table_grad.rows);
     const SortShape s = sort_shape(ids.count, table_grad.rows);
     SortArgs a = {};
@@ -625,7 +851,18 @@ hipError_t launch_embedding_grad(const RowMatrix& grad_out, const TokenIds& ids,
         return (uint32_t)std::min<uint64_t>(kClearBlocks, clear.end - clear.first);
     };
     hipError_t e;
-    for (uint32_t pass = 0; pass < s.passes; ++pass) {
+    if (ids.count <= kOneTokens) {
+        a.keys_out = w.keys[0];
+        a.order_out = w.order[0];
+        a.named = nullptr;
+        const uint32_t more = share(true);
+        hipLaunchKernelGGL((ids.wide ? sort_one_kernel<true> : sort_one_kernel<false>), dim3(1u + more), dim3(kOneThreads), 0, stream, a, clear, s.passes);
+        e = hipGetLastError();
+        if (e != hipSuccess) return e;
+        a.keys = a.keys_out;
+        a.order = a.order_out;
+    }
+    for (uint32_t pass = 0; ids.count > kOneTokens && pass < s.passes; ++pass) {
         a.keys_out = w.keys[pass & 1u];
         a.order_out = w.order[pass & 1u];
         a.shift = pass * s.bits;

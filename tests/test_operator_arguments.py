@@ -39,7 +39,7 @@ def test_workspace_sizes():
     assert mq.mqg_embedding_grad_workspace_bytes(0, 64, 100) == 0
     grown = [mq.mqg_embedding_grad_workspace_bytes(n, 64, 50000) for n in (1, 1000, 100_000, 10_000_000)]
     assert grown == sorted(grown) and all(b % 16 == 0 for b in grown)
-    for bad in ((1 << 31, 64, 100), (10, 0, 100), (10, (1 << 24) + 1, 100), (10, 64, 0), (10, 64, 1 << 31)):
+    for bad in ((1 << 31, 64, 100), (10, 0, 100), (10, (1 << 20) + 1, 100), (10, 64, 0), (10, 64, 1 << 31)):
         assert mq.mqg_embedding_grad_workspace_bytes(*bad) == 0
 
 
@@ -151,7 +151,7 @@ def grad(g=rows(A, 4), ids=tokens(), dim=16, out=rows(B), accumulate=0, workspac
 
 def test_embedding_arguments_are_checked():
     for call in (lookup, grad):
-        for dim in (0, (1 << 24) + 1):
+        for dim in (0, (1 << 20) + 1):
             assert call(dim=dim) == mq.MQG_EINVAL
         assert call(ids=None) == mq.MQG_EINVAL
         assert call(out=None) == mq.MQG_EINVAL
@@ -181,10 +181,12 @@ def test_embedding_arguments_are_checked():
     assert grad(out=rows(B, 0)) == mq.MQG_EINVAL
     assert grad(out=rows(B, 8, 15)) == mq.MQG_EINVAL
     assert grad(out=rows(A + 64)) == mq.MQG_EINVAL                       # over grad_out
-    assert grad(workspace=None) == mq.MQG_EINVAL
-    assert grad(workspace=0x100008) == mq.MQG_EALIGN
+    many = dict(g=rows(A, 1000), ids=tokens(count=1000))                 # a few positions need no workspace
+    assert mq.mqg_embedding_grad_workspace_bytes(1000, 16, 8) > 0
+    assert grad(workspace=None, **many) == mq.MQG_EINVAL
+    assert grad(workspace=0x100008, **many) == mq.MQG_EALIGN
     for over in (A, 0x1000, B):
-        assert grad(workspace=over) == mq.MQG_EINVAL
+        assert grad(workspace=over, **many) == mq.MQG_EINVAL
     assert lookup(ids=tokens(None, 0), out=rows(None, 0)) == mq.MQG_OK    # no tokens: nothing to do
     assert grad(g=rows(None, 0), ids=tokens(None, 0), accumulate=1, workspace=None) == mq.MQG_OK
 
