@@ -773,8 +773,7 @@ mqg_status mqg_clip_global_norm(const mqg_clip_item* items, uint32_t count, doub
     if (misaligned8(norm_out) || misaligned8(workspace)) return MQG_EALIGN;
     st = clip_items(items, count, max_norm, norm_out, workspace, mqg_global_norm_workspace_bytes(count));
     if (st != MQG_OK) return st;
-    hipError_t err = mqg::launch_global_norm(items, count, static_cast<double*>(workspace), norm_out, static_cast<hipStream_t>(stream));
-    if (err == hipSuccess) err = mqg::launch_clip(items, count, norm_out, max_norm, static_cast<hipStream_t>(stream));
+    const hipError_t err = mqg::launch_clip_global_norm(items, count, max_norm, static_cast<double*>(workspace), norm_out, static_cast<hipStream_t>(stream));
     return err == hipSuccess ? MQG_OK : MQG_ELAUNCH;
 }
 

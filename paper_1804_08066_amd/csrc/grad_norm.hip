@@ -8,6 +8,7 @@
 // are added in a fixed order: equal inputs give equal bits.  Both passes are bound by memory: the norm reads every value
 // once, clipping reads it once more and writes it.
 
+#include <algorithm>
 #include <type_traits>
 
 #include "kernels.h"
@@ -19,7 +20,9 @@ namespace {
 using namespace values;
 
 constexpr uint32_t kThreads = 256;
-constexpr uint32_t kPiece = 8192;   // values of a tensor that a workgroup takes at a time
+// Values of a tensor that a workgroup takes at a time.  (1.2 G half-precision values clipped into fp32, pieces of 2048, 4096, 8192 and
+// 16384: 1645, 1567, 1677 and 1648 us.)
+constexpr uint32_t kPiece = 4096;
 
 // which of the tensors a piece belongs to: starts[k] <= piece < starts[k + 1], as in tensor_of_block, for more than 64
 template <uint32_t ENTRIES>
@@ -35,8 +38,8 @@ __device__ __forceinline__ uint32_t tensor_of_piece(const uint32_t (&starts)[ENT
     return passed - 1u;   // starts[0] is 0: at least one
 }
 
-// this lane's share of the squares of x[0 .. count), count <= kPiece
-template <int DTYPE>
+// this lane's share of the squares of x[0 .. count), count <= kPiece; ONCE: with streaming loads
+template <int DTYPE, bool ONCE>
 __device__ __forceinline__ double piece_squares(const void* x, const uint32_t count) {
     constexpr int V = DTYPE == kF32 ? 4 : 8;
     constexpr uint32_t kRow = kThreads * V, kRows = kPiece / kRow;
@@ -44,7 +47,10 @@ __device__ __forceinline__ double piece_squares(const void* x, const uint32_t co
     if (count == kPiece) {
         Pack<DTYPE, V> t[kRows];
 #pragma unroll
-        for (uint32_t r = 0; r < kRows; ++r) t[r].load_once(at<DTYPE>(x, r * kRow + threadIdx.x * V));
+        for (uint32_t r = 0; r < kRows; ++r) {
+            if constexpr (ONCE) t[r].load_once(at<DTYPE>(x, r * kRow + threadIdx.x * V));
+            else t[r].load(at<DTYPE>(x, r * kRow + threadIdx.x * V));
+        }
 #pragma unroll
         for (uint32_t r = 0; r < kRows; ++r) {
             float v[V];
@@ -74,6 +80,8 @@ __device__ __forceinline__ double workgroup_sum(double acc) {
     return t;
 }
 
+// The workgroups take pieces in turn: a partial sum of each.
+template <bool ONCE>
 __global__ __launch_bounds__(kThreads) void norm_partial_kernel(const NormTable b, double* __restrict__ partials) {
     double acc = 0.0;
     for (uint32_t piece = blockIdx.x; piece < b.pieces; piece += gridDim.x) {
@@ -82,17 +90,28 @@ __global__ __launch_bounds__(kThreads) void norm_partial_kernel(const NormTable 
         const uint64_t left = b.n[k] - base;
         const uint32_t count = left < kPiece ? (uint32_t)left : kPiece;
         const void* x = b.data[k];
-        acc += with_dtype(b.dtype[k], [&](auto d) { return piece_squares<d>(at<d>(x, base), count); });
+        acc += with_dtype(b.dtype[k], [&](auto d) { return piece_squares<d, ONCE>(at<d>(x, base), count); });
     }
     const double t = workgroup_sum(acc);
     if (threadIdx.x == 0u) partials[blockIdx.x] = t;
 }
 
-__global__ __launch_bounds__(kThreads) void norm_finish_kernel(const double* __restrict__ partials, const uint32_t count, double* __restrict__ norm) {
+// in every lane of the workgroup
+__device__ __forceinline__ double norm_of_partials(const double* __restrict__ partials, const uint32_t count) {
     double acc = 0.0;
-    for (uint32_t i = threadIdx.x; i < count; i += kThreads) acc += partials[i];
-    const double t = workgroup_sum(acc);
-    if (threadIdx.x == 0u) *norm = __builtin_sqrt(t);
+    constexpr uint32_t kAhead = 8;
+    for (uint32_t i = threadIdx.x; i < count; i += kAhead * kThreads) {
+        double t[kAhead];
+#pragma unroll
+        for (uint32_t j = 0; j < kAhead; ++j) t[j] = i + j * kThreads < count ? partials[i + j * kThreads] : 0.0;
+#pragma unroll
+        for (uint32_t j = 0; j < kAhead; ++j) acc += t[j];
+    }
+    return __builtin_sqrt(workgroup_sum(acc));
+}
+__global__ __launch_bounds__(kThreads) void norm_finish_kernel(const double* __restrict__ partials, const uint32_t count, double* __restrict__ norm) {
+    const double n = norm_of_partials(partials, count);
+    if (threadIdx.x == 0u) *norm = n;
 }
 
 // a norm that is not a number makes the factor one too: nothing hides it
@@ -121,8 +140,19 @@ __device__ __forceinline__ void clip_piece(const void* x, void* y, const uint32_
     for (uint32_t i = threadIdx.x; i < count; i += kThreads) store_one<OUT>(y, i, load_one<IN>(x, i) * c);
 }
 
-__global__ __launch_bounds__(kThreads) void clip_kernel(const ClipTable b, const double* __restrict__ norm, const double max_norm) {
-    const float c = clip_factor(*norm, max_norm);
+// A workgroup for every piece.  (2048 that take pieces in turn: 1745 us instead of 1677 for 1.2 G values in pieces of 8192.)
+// few != 0: that many partial sums stand in for the norm, and every workgroup adds them up as norm_finish_kernel does; the first leaves
+// the norm in *norm.
+__global__ __launch_bounds__(kThreads) void clip_kernel(const ClipTable b, const double* __restrict__ partials, const uint32_t few, double* __restrict__ norm,
+                                                        const double max_norm) {
+    double n;
+    if (few != 0u) {
+        n = norm_of_partials(partials, few);
+        if (blockIdx.x == 0u && threadIdx.x == 0u) *norm = n;
+    } else {
+        n = *norm;
+    }
+    const float c = clip_factor(n, max_norm);
     for (uint32_t piece = blockIdx.x; piece < b.pieces; piece += gridDim.x) {
         const uint32_t k = tensor_of_piece(b.start, b.count, piece);
         const uint64_t base = (uint64_t)(piece - b.start[k]) * kPiece;
@@ -130,13 +160,17 @@ __global__ __launch_bounds__(kThreads) void clip_kernel(const ClipTable b, const
         const uint32_t count = left < kPiece ? (uint32_t)left : kPiece;
         const void* x = b.data[k];
         void* y = b.out[k];
+        if (c == 1.0f && x == y) continue;   // in place and below the norm: every value is its own
         with_dtype(b.dtype[k], [&](auto in) {
             with_dtype(b.out_dtype[k], [&](auto out) { clip_piece<in, out>(at<in>(x, base), at<out>(y, base), count, c); });
         });
     }
 }
 
-uint32_t blocks_of(uint32_t pieces) { return pieces < kNormBlocks ? pieces : kNormBlocks; }
+constexpr uint32_t kMaxBlocks = 1u << 23;   // a launch holds less than 2^32 lanes
+// So few partial sums are added up by every workgroup of the clipping kernel, without a launch in between (1.07 M values in ten tensors:
+// a launch of 4 us less).
+constexpr uint32_t kFewPartials = 512;
 
 // fills `b` with the tensors from items[first] on, as many as fit; returns the next one
 template <class Table, class F>
@@ -162,23 +196,34 @@ uint32_t fill_table(Table& b, const mqg_clip_item* items, uint32_t first, uint32
 
 uint64_t norm_max_values() { return ((uint64_t)0x7FFFFFFF - MQG_MAX_NORM_TENSORS) * kPiece; }   // pieces of a launch fit 31 bits
 
-hipError_t launch_global_norm(const mqg_clip_item* items, uint32_t count, double* partials, double* norm, hipStream_t stream) {
+// the partial sums of all tensors; *stored: how many
+static hipError_t launch_partials(const mqg_clip_item* items, uint32_t count, bool once, double* partials, uint32_t* stored, hipStream_t stream) {
     NormTable b;
-    uint32_t stored = 0;
+    *stored = 0;
     for (uint32_t i = 0; i < count;) {
         i = fill_table(b, items, i, count, [](uint32_t, const mqg_clip_item&) {});
         if (b.pieces == 0) continue;
-        const uint32_t blocks = blocks_of(b.pieces);
-        hipLaunchKernelGGL(norm_partial_kernel, dim3(blocks), dim3(kThreads), 0, stream, b, partials + stored);
+        const uint32_t blocks = std::min(b.pieces, kNormBlocks);
+        hipLaunchKernelGGL((once ? norm_partial_kernel<true> : norm_partial_kernel<false>), dim3(blocks), dim3(kThreads), 0, stream, b, partials + *stored);
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
-        stored += blocks;
+        *stored += blocks;
     }
+    return hipSuccess;
+}
+static hipError_t launch_finish(const double* partials, uint32_t stored, double* norm, hipStream_t stream) {
     hipLaunchKernelGGL(norm_finish_kernel, dim3(1), dim3(kThreads), 0, stream, partials, stored, norm);
     return hipGetLastError();
 }
 
-hipError_t launch_clip(const mqg_clip_item* items, uint32_t count, const double* norm, double max_norm, hipStream_t stream) {
+hipError_t launch_global_norm(const mqg_clip_item* items, uint32_t count, double* partials, double* norm, hipStream_t stream) {
+    uint32_t stored;
+    const hipError_t e = launch_partials(items, count, true, partials, &stored, stream);
+    return e == hipSuccess ? launch_finish(partials, stored, norm, stream) : e;
+}
+
+static hipError_t launch_clip_pieces(const mqg_clip_item* items, uint32_t count, const double* partials, uint32_t few, double* norm, double max_norm,
+                                     hipStream_t stream) {
     ClipTable b;
     for (uint32_t i = 0; i < count;) {
         i = fill_table(b, items, i, count, [&](uint32_t k, const mqg_clip_item& it) {
@@ -186,11 +231,29 @@ hipError_t launch_clip(const mqg_clip_item* items, uint32_t count, const double*
             b.out_dtype[k] = (uint8_t)it.out_dtype;
         });
         if (b.pieces == 0) continue;
-        hipLaunchKernelGGL(clip_kernel, dim3(blocks_of(b.pieces)), dim3(kThreads), 0, stream, b, norm, max_norm);
+        hipLaunchKernelGGL(clip_kernel, dim3(std::min(b.pieces, kMaxBlocks)), dim3(kThreads), 0, stream, b, partials, few, norm, max_norm);
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
+        few = 0;   // the first launch has left the norm
     }
     return hipSuccess;
+}
+
+hipError_t launch_clip(const mqg_clip_item* items, uint32_t count, const double* norm, double max_norm, hipStream_t stream) {
+    return launch_clip_pieces(items, count, nullptr, 0, const_cast<double*>(norm), max_norm, stream);   // which is only read
+}
+
+hipError_t launch_clip_global_norm(const mqg_clip_item* items, uint32_t count, double max_norm, double* partials, double* norm, hipStream_t stream) {
+    uint64_t bytes = 0;
+    for (uint32_t i = 0; i < count; ++i) bytes += items[i].n * bytes_of(items[i].dtype);
+    // Values that clipping may find in the last-level cache are read with ordinary loads: 0.2, 0.5 and 0.8 GB of half-precision values into
+    // fp32 took 182, 308 and 686 us with streaming loads and take 170, 291 and 676; 2.4 GB 1567 and 1580.
+    uint32_t stored;
+    hipError_t e = launch_partials(items, count, bytes > (1ull << 30), partials, &stored, stream);
+    if (e != hipSuccess) return e;
+    const bool few = stored > 0 && stored <= kFewPartials;
+    if (!few) e = launch_finish(partials, stored, norm, stream);
+    return e == hipSuccess ? launch_clip_pieces(items, count, partials, few ? stored : 0u, norm, max_norm, stream) : e;
 }
 
 }  // namespace mqg

@@ -253,6 +253,7 @@ uint64_t norm_max_values();              // of all tensors together
 // `items` are checked; items without values are skipped
 hipError_t launch_global_norm(const mqg_clip_item* items, uint32_t count, double* partials, double* norm, hipStream_t stream);
 hipError_t launch_clip(const mqg_clip_item* items, uint32_t count, const double* norm, double max_norm, hipStream_t stream);
+hipError_t launch_clip_global_norm(const mqg_clip_item* items, uint32_t count, double max_norm, double* partials, double* norm, hipStream_t stream);
 
 // embedding.hip
 struct RowMatrix {

@@ -267,6 +267,13 @@ struct Entries {
     decltype(&mqg_quantize_minmax_tensors) quantize_minmax_tensors;
     decltype(&mqg_aggregate_update_tensors) aggregate_update_tensors;
     decltype(&mqg_aggregate_update_minmax_tensors) aggregate_update_minmax_tensors;
+    decltype(&mqg_global_norm) global_norm;
+    decltype(&mqg_clip_by_norm) clip_by_norm;
+    decltype(&mqg_clip_global_norm) clip_global_norm;
+    decltype(&mqg_embedding) embedding;
+    decltype(&mqg_embedding_grad) embedding_grad;
+    decltype(&mqg_global_norm_workspace_bytes) global_norm_workspace_bytes;
+    decltype(&mqg_embedding_grad_workspace_bytes) embedding_grad_workspace_bytes;
 };
 constexpr Py_ssize_t kEntries = sizeof(Entries) / sizeof(void*);
 Entries lib;
@@ -448,6 +455,163 @@ PyObject* update_tensors(PyObject*, PyObject* const* a, Py_ssize_t argc) {
     });
 }
 
+// ---- norm, clipping, embedding ------------------------------------------------------------------------
+// These calls refuse tensors of another device than the current one.
+struct Device {
+    long index = -1;
+    Device() {
+        if (current_device == nullptr) throw Reject{};
+        PyObject* d = PyObject_CallNoArgs(current_device);
+        if (d != nullptr) index = PyLong_AsLong(d);
+        Py_XDECREF(d);
+        if (PyErr_Occurred()) throw Reject{};
+    }
+    const at::Tensor& here(const at::Tensor& t) const {
+        if (t.get_device() != index) throw Reject{};
+        return t;
+    }
+};
+mqg_dtype dtype_of(const at::Tensor& t) {
+    switch (t.scalar_type()) {
+        case at::kFloat: return MQG_FLOAT32;
+        case at::kHalf: return MQG_FLOAT16;
+        case at::kBFloat16: return MQG_BFLOAT16;
+        default: throw Reject{};
+    }
+}
+const at::Tensor& any(PyObject* o) {
+    if (!THPVariable_CheckExact(o)) throw Reject{};
+    const at::Tensor& t = THPVariable_Unpack(o);
+    if (!t.defined() || !t.is_cuda()) throw Reject{};
+    return t;
+}
+const at::Tensor& values(PyObject* o, const Device& d) {
+    const at::Tensor& t = d.here(any(o));
+    if (!t.is_contiguous()) throw Reject{};
+    return t;
+}
+// scratch memory of at least need() bytes; the tensor's type is of no interest
+template <class F>
+void* scratch(PyObject* o, const Device& d, F need) {
+    const at::Tensor& t = values(o, d);
+    if (lib.global_norm == nullptr || (size_t)t.nbytes() < need()) throw Reject{};
+    return t.data_ptr();
+}
+double number(PyObject* o) {
+    if (PyFloat_CheckExact(o)) return PyFloat_AS_DOUBLE(o);
+    throw Reject{};
+}
+int64_t integer(PyObject* o) {
+    if (!PyLong_CheckExact(o)) throw Reject{};
+    const long long v = PyLong_AsLongLong(o);
+    if (v == -1 && PyErr_Occurred()) throw Reject{};
+    return v;
+}
+std::vector<mqg_clip_item> clip_items(PyObject* tensors, PyObject* outputs, const Device& d) {
+    const Items in(tensors), out(outputs == Py_None ? tensors : outputs, in.count);
+    if (in.count == 0 || in.count > (Py_ssize_t)MQG_MAX_NORM_TENSORS) throw Reject{};
+    std::vector<mqg_clip_item> items((size_t)in.count);
+    for (Py_ssize_t i = 0; i < in.count; ++i) {
+        const at::Tensor& x = values(in.at[i], d);
+        const at::Tensor& y = outputs == Py_None ? x : values(out.at[i], d);
+        if (x.numel() != y.numel()) throw Reject{};
+        items[(size_t)i] = mqg_clip_item{x.data_ptr(), y.data_ptr(), (uint64_t)x.numel(), dtype_of(x), dtype_of(y)};
+    }
+    return items;
+}
+double* one_double(PyObject* o, const Device& d) {
+    const at::Tensor& t = d.here(plain(o, at::kDouble));
+    if (t.numel() < 1) throw Reject{};
+    return static_cast<double*>(t.data_ptr());
+}
+// norm(tensors, workspace, norm_out, stream) -> status
+PyObject* norm(PyObject*, PyObject* const* a, Py_ssize_t argc) {
+    return guarded([&]() -> PyObject* {
+        if (argc != 4) throw Reject{};
+        const Device d;
+        const std::vector<mqg_clip_item> items = clip_items(a[0], Py_None, d);
+        void* ws = scratch(a[1], d, [&] { return lib.global_norm_workspace_bytes((uint32_t)items.size()); });
+        double* out = one_double(a[2], d);
+        void* stream = stream_of(a[3]);
+        return status_of([&] { return lib.global_norm(items.data(), (uint32_t)items.size(), ws, out, stream); });
+    });
+}
+// clip_by_norm(tensors, outputs, norm, max_norm, stream) -> status
+PyObject* clip_by_norm(PyObject*, PyObject* const* a, Py_ssize_t argc) {
+    return guarded([&]() -> PyObject* {
+        if (argc != 5) throw Reject{};
+        const Device d;
+        const std::vector<mqg_clip_item> items = clip_items(a[0], a[1], d);
+        const double* at = one_double(a[2], d);
+        const double most = number(a[3]);
+        void* stream = stream_of(a[4]);
+        return status_of([&] { return lib.clip_by_norm(items.data(), (uint32_t)items.size(), at, most, stream); });
+    });
+}
+// clip_global_norm(tensors, outputs, max_norm, workspace, norm_out, stream) -> status
+PyObject* clip_global_norm(PyObject*, PyObject* const* a, Py_ssize_t argc) {
+    return guarded([&]() -> PyObject* {
+        if (argc != 6) throw Reject{};
+        const Device d;
+        const std::vector<mqg_clip_item> items = clip_items(a[0], a[1], d);
+        const double most = number(a[2]);
+        void* ws = scratch(a[3], d, [&] { return lib.global_norm_workspace_bytes((uint32_t)items.size()); });
+        double* out = one_double(a[4], d);
+        void* stream = stream_of(a[5]);
+        return status_of([&] { return lib.clip_global_norm(items.data(), (uint32_t)items.size(), most, ws, out, stream); });
+    });
+}
+// rows of one stride: two dimensions, or more that are contiguous
+mqg_rows rows_of(PyObject* o, const Device& d, uint64_t* dim) {
+    const at::Tensor& t = d.here(any(o));
+    if (t.dim() == 2) {
+        if (t.size(1) > 1 && t.stride(1) != 1) throw Reject{};
+    } else if (t.dim() < 2 || !t.is_contiguous()) {
+        throw Reject{};
+    }
+    const int64_t width = t.size(-1);
+    if (width < 1) throw Reject{};
+    *dim = (uint64_t)width;
+    return mqg_rows{t.data_ptr(), (uint64_t)(t.dim() == 2 ? t.size(0) : t.numel() / width), (uint64_t)(t.dim() == 2 ? t.stride(0) : width), dtype_of(t)};
+}
+mqg_tokens tokens_of(PyObject* o, const Device& d, PyObject* first_row, PyObject* padding) {
+    const at::Tensor& t = values(o, d);
+    if (t.scalar_type() != at::kInt && t.scalar_type() != at::kLong) throw Reject{};
+    return mqg_tokens{t.data_ptr(), (uint64_t)t.numel(), t.scalar_type() == at::kLong ? MQG_INDEX64 : MQG_INDEX32, integer(first_row),
+                      padding == Py_None ? INT64_MIN : integer(padding)};
+}
+// embedding(table, ids, scale, first_row, out, stream) -> status
+PyObject* embedding(PyObject*, PyObject* const* a, Py_ssize_t argc) {
+    return guarded([&]() -> PyObject* {
+        if (argc != 6) throw Reject{};
+        const Device d;
+        uint64_t dim, out_dim;
+        const mqg_rows table = rows_of(a[0], d, &dim), out = rows_of(a[4], d, &out_dim);
+        const mqg_tokens ids = tokens_of(a[1], d, a[3], Py_None);
+        const float scale = real(a[2]);
+        if (out_dim != dim || out.rows != ids.count || dim > MQG_MAX_ROW_DIM) throw Reject{};
+        void* stream = stream_of(a[5]);
+        return status_of([&] { return lib.embedding(&table, &ids, (uint32_t)dim, scale, &out, stream); });
+    });
+}
+// embedding_grad(grad_out, ids, rows, scale, first_row, padding, out, accumulate, workspace, stream) -> status
+PyObject* embedding_grad(PyObject*, PyObject* const* a, Py_ssize_t argc) {
+    return guarded([&]() -> PyObject* {
+        if (argc != 10) throw Reject{};
+        const Device d;
+        uint64_t dim, out_dim;
+        const mqg_rows grad = rows_of(a[0], d, &dim), out = rows_of(a[6], d, &out_dim);
+        const mqg_tokens ids = tokens_of(a[1], d, a[4], a[5]);
+        const float scale = real(a[3]);
+        if (out_dim != dim || grad.rows != ids.count || out.rows != whole(a[2]) || dim > MQG_MAX_ROW_DIM) throw Reject{};
+        const int accumulate = PyObject_IsTrue(a[7]);
+        if (accumulate < 0) throw Reject{};
+        void* ws = scratch(a[8], d, [&] { return lib.embedding_grad_workspace_bytes(ids.count, (uint32_t)dim, out.rows); });
+        void* stream = stream_of(a[9]);
+        return status_of([&] { return lib.embedding_grad(&grad, &ids, (uint32_t)dim, scale, &out, accumulate, ws, stream); });
+    });
+}
+
 template <class F>
 PyCFunction fast(F f) { return reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(f)); }
 PyMethodDef methods[] = {
@@ -463,6 +627,11 @@ PyMethodDef methods[] = {
     {"dequantize_update", fast(dequantize_update), METH_FASTCALL, nullptr},
     {"quantize_tensors", fast(quantize_tensors), METH_FASTCALL, nullptr},
     {"update_tensors", fast(update_tensors), METH_FASTCALL, nullptr},
+    {"norm", fast(norm), METH_FASTCALL, nullptr},
+    {"clip_by_norm", fast(clip_by_norm), METH_FASTCALL, nullptr},
+    {"clip_global_norm", fast(clip_global_norm), METH_FASTCALL, nullptr},
+    {"embedding", fast(embedding), METH_FASTCALL, nullptr},
+    {"embedding_grad", fast(embedding_grad), METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr},
 };
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_marshal", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};

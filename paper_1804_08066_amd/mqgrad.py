@@ -226,13 +226,16 @@ class _NoTables:
     checks make every table."""
     pointers = stream = quantize_items = update_items = staticmethod(lambda *args: None)
     bind = quantize = quantize_minmax = update = requantize = dequantize_update = quantize_tensors = update_tensors = pointers
+    norm = clip_by_norm = clip_global_norm = embedding = embedding_grad = pointers
 
 
 # the entries that the native module calls itself, in its order
 _CALLED = ("mqg_quantize_mode", "mqg_quantize_minmax", "mqg_quantize_minmax_tensor", "mqg_aggregate_update_from",
            "mqg_aggregate_update_minmax", "mqg_aggregate_update_minmax_tensor", "mqg_aggregate_requantize_mode",
            "mqg_aggregate_requantize_minmax", "mqg_aggregate_requantize_minmax_tensor", "mqg_dequantize_update", "mqg_quantize_tensors_mode",
-           "mqg_quantize_minmax_tensors", "mqg_aggregate_update_tensors", "mqg_aggregate_update_minmax_tensors")
+           "mqg_quantize_minmax_tensors", "mqg_aggregate_update_tensors", "mqg_aggregate_update_minmax_tensors", "mqg_global_norm", "mqg_clip_by_norm",
+           "mqg_clip_global_norm", "mqg_embedding", "mqg_embedding_grad", "mqg_global_norm_workspace_bytes",
+           "mqg_embedding_grad_workspace_bytes")
 _TAKES_TABLES = ("mqg_aggregate_update_from", "mqg_aggregate_requantize_mode", "mqg_aggregate_mean", "mqg_quantize_tensors_mode",
                  "mqg_aggregate_update_tensors", "mqg_aggregate_update_minmax_tensors", "mqg_quantize_minmax_tensors",
                  "mqg_aggregate_update_minmax", "mqg_aggregate_requantize_minmax", "mqg_aggregate_update_minmax_tensor",
@@ -803,18 +806,19 @@ def _one_device(tensors):
             raise ValueError("all tensors must be on the current device, cuda:%d" % device)
 
 
-def _scratch(workspace, need, stream, device, what="workspace"):
-    """A caller's workspace, checked, or one of this call's own, which the stream keeps until its work is done."""
-    if workspace is None:
-        workspace = torch.empty(need, dtype=torch.uint8, device=device)
-        if stream is not None:
-            workspace.record_stream(stream)
-        return workspace
-    if not (isinstance(workspace, torch.Tensor) and workspace.is_cuda and workspace.is_contiguous()):
-        raise TypeError("%s must be a contiguous CUDA tensor" % what)
-    if workspace.numel() * workspace.element_size() < need:
-        raise ValueError("%s must hold %d bytes" % (what, need))
+def _scratch(need, stream, device):
+    """A workspace of a call's own, which the stream keeps until its work is done."""
+    workspace = torch.empty(need, dtype=torch.uint8, device=device)
+    if stream is not None and workspace.is_cuda:
+        workspace.record_stream(stream)
     return workspace
+
+
+def _check_scratch(workspace, need):
+    if not (isinstance(workspace, torch.Tensor) and workspace.is_cuda and workspace.is_contiguous()):
+        raise TypeError("workspace must be a contiguous CUDA tensor")
+    if workspace.numel() * workspace.element_size() < need:
+        raise ValueError("workspace must hold %d bytes" % need)
 
 
 def _clip_items(tensors, outputs):
@@ -840,24 +844,36 @@ def mqg_global_norm(tensors, workspace=None, norm_out=None, stream=None):
     """The L2 norm of all the tensors together (float32, float16 and bfloat16, in any mix), reproducible to the bit, into a
     one-element float64 device tensor.  `workspace`: a device tensor of at least mqg_global_norm_workspace_bytes(len(tensors))
     bytes (allocated here when not given)."""
-    L, count = lib(), len(tensors)
-    items = _clip_items(tensors, None)
-    return _norm_call(L.mqg_global_norm, "mqg_global_norm", tensors, [], items, (count,), workspace, norm_out, stream)
+    workspace, norm_out = _norm_buffers(tensors, workspace, norm_out, stream)
+    st = _marshal.norm(tensors, workspace, norm_out, stream)
+    if st is None:
+        _check_norm_buffers(tensors, workspace, norm_out)
+        items = _clip_items(tensors, None)
+        st = _lib.mqg_global_norm(items, len(tensors), workspace.data_ptr(), norm_out.data_ptr(), _stream_handle(stream))
+    if st != MQG_OK:
+        raise MqgError(st, "mqg_global_norm")
+    return norm_out
 
 
-def _norm_call(entry, name, tensors, outputs, items, args, workspace, norm_out, stream):
-    dev = tensors[0].device if len(tensors) else "cuda"
-    if norm_out is None:
-        norm_out = torch.empty(1, dtype=torch.float64, device=dev)
+def _norm_buffers(tensors, workspace, norm_out, stream):
+    _lib or lib()
+    if workspace is None or norm_out is None:
+        dev = tensors[0].device if len(tensors) else "cuda"
+        if workspace is None:
+            workspace = _scratch(mqg_global_norm_workspace_bytes(len(tensors)), stream, dev)
+        if norm_out is None:
+            norm_out = torch.empty(1, dtype=torch.float64, device=dev)
+    return workspace, norm_out
+
+
+def _check_norm_buffers(tensors, workspace, norm_out):
     _check(norm_out, torch.float64, "norm_out")
     if norm_out.numel() < 1:
         raise ValueError("norm_out must hold one value")
-    workspace = _scratch(workspace, mqg_global_norm_workspace_bytes(len(tensors)), stream, dev)
-    _one_device([*tensors, *outputs, workspace, norm_out])
-    st = entry(items, *args, workspace.data_ptr(), norm_out.data_ptr(), _stream_handle(stream))
-    if st != MQG_OK:
-        raise MqgError(st, name)
-    return norm_out
+    _check_scratch(workspace, mqg_global_norm_workspace_bytes(len(tensors)))
+    for k, t in enumerate(tensors):
+        _values(t, "tensors[%d]" % k)
+    _one_device([*tensors, workspace, norm_out])
 
 
 def _outputs(tensors, outputs):
@@ -872,12 +888,15 @@ def mqg_clip_by_norm(tensors, norm, max_norm, outputs=None, stream=None):
     """Every tensor times min(1, max_norm / norm), for a norm that is on the device already (one float64 value); into `outputs`,
     of any of the three types, or in place.  Returns the list of outputs."""
     outputs = _outputs(tensors, outputs)
-    L, items = lib(), _clip_items(tensors, outputs)
-    _check(norm, torch.float64, "norm")
-    if norm.numel() < 1:
-        raise ValueError("norm must hold one value")
-    _one_device([*tensors, *outputs, norm])
-    st = L.mqg_clip_by_norm(items, len(tensors), norm.data_ptr(), max_norm, _stream_handle(stream))
+    _lib or lib()
+    st = _marshal.clip_by_norm(tensors, outputs, norm, max_norm, stream)
+    if st is None:
+        items = _clip_items(tensors, outputs)
+        _check(norm, torch.float64, "norm")
+        if norm.numel() < 1:
+            raise ValueError("norm must hold one value")
+        _one_device([*tensors, *outputs, norm])
+        st = _lib.mqg_clip_by_norm(items, len(tensors), norm.data_ptr(), max_norm, _stream_handle(stream))
     if st != MQG_OK:
         raise MqgError(st, "mqg_clip_by_norm")
     return outputs
@@ -887,9 +906,16 @@ def mqg_clip_global_norm(tensors, max_norm, outputs=None, workspace=None, norm_o
     """mqg_global_norm of all the tensors, and every tensor scaled by min(1, max_norm / norm) into `outputs`, of any of the three
     types, or in place.  Returns (outputs, norm)."""
     outputs = _outputs(tensors, outputs)
-    L, items = lib(), _clip_items(tensors, outputs)
-    return outputs, _norm_call(L.mqg_clip_global_norm, "mqg_clip_global_norm", tensors, outputs, items, (len(tensors), max_norm), workspace,
-                               norm_out, stream)
+    workspace, norm_out = _norm_buffers(tensors, workspace, norm_out, stream)
+    st = _marshal.clip_global_norm(tensors, outputs, max_norm, workspace, norm_out, stream)
+    if st is None:
+        _check_norm_buffers(tensors, workspace, norm_out)
+        items = _clip_items(tensors, outputs)
+        _one_device(outputs)
+        st = _lib.mqg_clip_global_norm(items, len(tensors), max_norm, workspace.data_ptr(), norm_out.data_ptr(), _stream_handle(stream))
+    if st != MQG_OK:
+        raise MqgError(st, "mqg_clip_global_norm")
+    return outputs, norm_out
 
 
 def _rows(t, what):
@@ -920,6 +946,13 @@ _NO_PADDING = -(1 << 63)
 def mqg_embedding(table, ids, scale=1.0, first_row=0, out=None, stream=None):
     """scale * table[ids - first_row], rows of zeros for tokens outside the table.  table: [rows, dim], rows at any stride; ids: int32 or
     int64, of any shape; out: [*ids.shape, dim] of any of the three types (allocated here, in the table's type, when not given)."""
+    _lib or lib()
+    if out is not None:
+        st = _marshal.embedding(table, ids, scale, first_row, out, stream)
+        if st == MQG_OK:
+            return out
+        if st is not None:
+            raise MqgError(st, "mqg_embedding")
     t, dim = _rows(table, "table")
     tokens = _tokens(ids, first_row, _NO_PADDING)
     if out is None:
@@ -928,7 +961,7 @@ def mqg_embedding(table, ids, scale=1.0, first_row=0, out=None, stream=None):
     if out_dim != dim or o.rows != tokens.count:
         raise ValueError("out must hold one row of the table for every token")
     _one_device([table, ids, out])
-    st = lib().mqg_embedding(C.byref(t), C.byref(tokens), dim, scale, C.byref(o), _stream_handle(stream))
+    st = _lib.mqg_embedding(C.byref(t), C.byref(tokens), dim, scale, C.byref(o), _stream_handle(stream))
     if st != MQG_OK:
         raise MqgError(st, "mqg_embedding")
     return out
@@ -943,6 +976,13 @@ def mqg_embedding_grad(grad_out, ids, rows, scale=1.0, first_row=0, padding_id=N
     grad_out's rows, summed in fp32 and reproducible to the bit.  Positions of padding_id add to no row.  out: [rows, dim] of any of the
     three types, overwritten, or with accumulate=True added to (allocated here, in grad_out's type, when not given).  `workspace`: a
     device tensor of at least mqg_embedding_grad_workspace_bytes(ids.numel(), dim, rows) bytes (allocated here when not given)."""
+    _lib or lib()
+    if out is not None and workspace is not None:
+        st = _marshal.embedding_grad(grad_out, ids, rows, scale, first_row, padding_id, out, accumulate, workspace, stream)
+        if st == MQG_OK:
+            return out
+        if st is not None:
+            raise MqgError(st, "mqg_embedding_grad")
     g, dim = _rows(grad_out, "grad_out")
     tokens = _tokens(ids, first_row, _NO_PADDING if padding_id is None else padding_id)
     if g.rows != tokens.count:
@@ -954,10 +994,13 @@ def mqg_embedding_grad(grad_out, ids, rows, scale=1.0, first_row=0, padding_id=N
     o, out_dim = _rows(out, "out")
     if out_dim != dim or o.rows != rows:
         raise ValueError("out must have %d rows of grad_out's width" % rows)
-    workspace = _scratch(workspace, mqg_embedding_grad_workspace_bytes(tokens.count, dim, rows), stream, out.device)
+    need = mqg_embedding_grad_workspace_bytes(tokens.count, dim, rows)
+    if workspace is None:
+        workspace = _scratch(need, stream, out.device)
+    _check_scratch(workspace, need)
     _one_device([grad_out, ids, out, workspace])
-    st = lib().mqg_embedding_grad(C.byref(g), C.byref(tokens), dim, scale, C.byref(o), 1 if accumulate else 0, workspace.data_ptr(),
-                                  _stream_handle(stream))
+    st = _lib.mqg_embedding_grad(C.byref(g), C.byref(tokens), dim, scale, C.byref(o), 1 if accumulate else 0, workspace.data_ptr(),
+                                 _stream_handle(stream))
     if st != MQG_OK:
         raise MqgError(st, "mqg_embedding_grad")
     return out

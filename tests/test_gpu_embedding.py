@@ -384,7 +384,11 @@ def test_the_servers_update_from_rows():
     check_grad(g, ids, params, rows, -lr / W, old=old)
 
 
-def test_binding_refusals():
+@pytest.mark.parametrize("native", [True, False])
+def test_binding_refusals(monkeypatch, native):
+    mq.lib()
+    if not native:
+        monkeypatch.setattr(mq, "_marshal", mq._NoTables)
     table = matrix(10, 16, 1)
     ids = torch.zeros(4, dtype=torch.int64, device=DEV)
     g = matrix(4, 16, 2)
@@ -417,3 +421,18 @@ def test_binding_refusals():
         mq.mqg_embedding_grad(g, ids, 4, out=g)
     with pytest.raises(mq.MqgError):
         mq.mqg_embedding_grad(g, ids, 10, out=torch.empty(1, 16, device=DEV).expand(10, 16))
+
+
+def test_every_form_of_argument_gives_the_same_results(monkeypatch):
+    """Whole numbers for scale, parameters, buffers of the call's own or given, and the binding without its native tables."""
+    table, ids, g = matrix(90, 40, 1), some_tokens("text", 2000, 90).to(DEV), matrix(2000, 40, 2)
+    looked, grad = mq.mqg_embedding(table, ids, scale=2.0), mq.mqg_embedding_grad(g, ids, 90, scale=2.0, padding_id=1)
+    for native in (True, False):
+        if not native:
+            monkeypatch.setattr(mq, "_marshal", mq._NoTables)
+        for scale in (2, 2.0):
+            assert torch.equal(mq.mqg_embedding(torch.nn.Parameter(table), ids, scale=scale), looked)
+            assert torch.equal(mq.mqg_embedding(table, ids, scale=scale, out=torch.zeros_like(looked)), looked)
+            assert torch.equal(mq.mqg_embedding_grad(g, ids, 90, scale=scale, padding_id=1), grad)
+            workspace = torch.empty(mq.mqg_embedding_grad_workspace_bytes(2000, 40, 90) // 4, dtype=torch.int32, device=DEV)
+            assert torch.equal(mq.mqg_embedding_grad(g, ids, 90, scale=scale, padding_id=1, out=torch.zeros_like(grad), workspace=workspace), grad)

@@ -5,6 +5,7 @@ sizes (32 per piece of a tensor and the pieces of a workgroup, the wave, the wor
 at most 300 * 2^-53 of itself and the root by half of that and its own rounding: 2e-14.
 Clipping: the factor is rounded to fp32 (2^-24), the product once (2^-24), the result to the output's type (eps / 2), and where
 that type's values are subnormal by half its smallest step."""
+import collections
 import math
 
 import numpy as np
@@ -254,7 +255,11 @@ def test_clipped_gradients_through_the_exchange():
     assert np.array_equal(params.cpu().numpy(), host)
 
 
-def test_binding_refusals():
+@pytest.mark.parametrize("native", [True, False])
+def test_binding_refusals(monkeypatch, native):
+    mq.lib()
+    if not native:
+        monkeypatch.setattr(mq, "_marshal", mq._NoTables)
     t = values(100, 1)
     with pytest.raises(TypeError):
         mq.mqg_global_norm([t, t.double()])
@@ -272,3 +277,25 @@ def test_binding_refusals():
         mq.mqg_clip_global_norm([t], -1.0)
     with pytest.raises(mq.MqgError):
         mq.mqg_clip_global_norm([t[:50]], 1.0, outputs=[t[25:75]])
+
+
+def test_every_form_of_argument_gives_the_same_results(monkeypatch):
+    """Lists, tuples and other sequences, parameters, whole numbers for max_norm, buffers of the call's own, and the binding without
+    its native tables."""
+    tensors = [values(3000, 1), values(50, 2, BF16)]
+    outputs = [torch.zeros(t.numel(), device=DEV) for t in tensors]
+    _, norm = mq.mqg_clip_global_norm(tensors, 0.25, outputs=outputs)
+    want, value = [o.clone() for o in outputs], norm.item()
+    for native in (True, False):
+        if not native:
+            monkeypatch.setattr(mq, "_marshal", mq._NoTables)
+        for wrap in (list, tuple, collections.UserList):
+            assert mq.mqg_global_norm(wrap(tensors)).item() == value
+            got, norm = mq.mqg_clip_global_norm(wrap(tensors), 0.25, outputs=wrap([torch.zeros_like(o) for o in outputs]))
+            assert norm.item() == value and all(torch.equal(a, b) for a, b in zip(got, want))
+            got = mq.mqg_clip_by_norm(wrap(tensors), norm, 0.25, outputs=wrap([torch.zeros_like(o) for o in outputs]))
+            assert all(torch.equal(a, b) for a, b in zip(got, want))
+        params = [torch.nn.Parameter(t.clone()) for t in tensors]
+        assert mq.mqg_global_norm(params).item() == value
+        kept, _ = mq.mqg_clip_global_norm([t.clone() for t in tensors], 1 << 20)
+        assert all(torch.equal(a, b) for a, b in zip(kept, tensors))
