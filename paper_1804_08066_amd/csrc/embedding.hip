@@ -30,21 +30,53 @@ __device__ __forceinline__ uint32_t row_of(const TokenIds& t, uint64_t i, uint64
 // fp32 are two stores of half a line each: the sums of 131072 half-precision rows took 386 us instead of 345.)
 constexpr int values_of(int in, int out) { return in == kF32 || out == kF32 ? 4 : 8; }
 
-// y[0 .. min(V, left)) <- v; once: with streaming stores
-template <int OUT, int V>
-__device__ __forceinline__ void store_values(void* y, const float (&v)[V], uint32_t left, bool once) {
-    if (left >= V) {
-        Pack<OUT, V> o;
+// A lane's V values of a row that begin at `col`.  Where fewer are left, the last V of the row: values that two lanes hold are the same
+// in both, so that a lane never reads or writes one by one (23694 rows of 455 values: their sums took 28 us with tails that are read
+// value by value, and take 12).  Rows of less than V values are read and written one by one.
+template <int V>
+struct Window {
+    uint32_t at, skip;      // first value; those before `col`, which another lane holds too
+    bool narrow;
+    __device__ __forceinline__ Window(uint32_t col, uint32_t dim) : at(dim < V ? 0u : min(col, dim - V)), skip(col - at), narrow(dim < V) {}
+    template <int DTYPE>
+    __device__ __forceinline__ void load(Pack<DTYPE, V>& t, const void* row, uint32_t dim) const {
+        if (narrow) t.load_some(row, dim);
+        else t.load(values::at<DTYPE>(row, at));
+    }
+    template <int DTYPE>
+    __device__ __forceinline__ void load_once(Pack<DTYPE, V>& t, const void* row, uint32_t dim) const {
+        if (narrow) t.load_some(row, dim);
+        else t.load_once(values::at<DTYPE>(row, at));
+    }
+    template <int DTYPE>
+    __device__ __forceinline__ void store_once(void* row, const float (&v)[V], uint32_t dim) const {
+        if (narrow) {
+            store_from<DTYPE>(row, v, 0u, dim);
+            return;
+        }
+        Pack<DTYPE, V> o;
         o.set(v);
-        if (once) o.store_once(y);
-        else o.store(y);
-        return;
+        o.store_once(values::at<DTYPE>(row, at));
     }
+    // the lane's own values only: what is added to an old value is added once
+    template <int DTYPE>
+    __device__ __forceinline__ void store_own(void* row, const float (&v)[V], uint32_t dim) const {
+        if (narrow || skip != 0u) {
+            store_from<DTYPE>(values::at<DTYPE>(row, at), v, skip, narrow ? dim : (uint32_t)V);
+            return;
+        }
+        Pack<DTYPE, V> o;
+        o.set(v);
+        o.store(values::at<DTYPE>(row, at));
+    }
+    template <int DTYPE>
+    static __device__ __forceinline__ void store_from(void* p, const float (&v)[V], uint32_t first, uint32_t end) {
 #pragma unroll
-    for (int i = 0; i < V; ++i) {
-        if ((uint32_t)i < left) store_one<OUT>(y, i, v[i]);
+        for (int i = 0; i < V; ++i) {
+            if ((uint32_t)i >= first && (uint32_t)i < end) store_one<DTYPE>(p, i, v[i]);
+        }
     }
-}
+};
 
 // ---- lookup ------------------------------------------------------------------------------------------
 // `1 << shift` lanes hold a row's (or a slice of a row's) values, V each, of kLookups rows at a time; the slices of a row
@@ -59,7 +91,7 @@ __global__ __launch_bounds__(kThreads) void embedding_kernel(const RowMatrix tab
     const uint32_t lane = threadIdx.x & ((1u << shift) - 1u), per = kThreads >> shift, block = blockIdx.x / slices;
     const uint32_t col = (((blockIdx.x - block * slices) << shift) + lane) * V;
     if (col >= dim) return;
-    const bool whole = col + V <= dim;
+    const Window<V> w(col, dim);
     const uint64_t step = (uint64_t)per * kLookups;
     for (uint64_t p = block * step + (threadIdx.x >> shift); p < ids.count; p += gridDim.x / slices * step) {
         uint32_t row[kLookups];
@@ -73,19 +105,16 @@ __global__ __launch_bounds__(kThreads) void embedding_kernel(const RowMatrix tab
 #pragma unroll
         for (uint32_t r = 0; r < kLookups; ++r) {
             if (!there[r]) continue;
-            const void* x = at<IN>(table.data, (uint64_t)row[r] * table.stride + col);
-            if (whole) t[r].load(x);
-            else t[r].load_some(x, dim - col);
+            w.load(t[r], at<IN>(table.data, (uint64_t)row[r] * table.stride), dim);
         }
 #pragma unroll
         for (uint32_t r = 0; r < kLookups; ++r) {
             if (p + r * per >= ids.count) break;
-            void* y = at<OUT>(out.data, (p + r * per) * out.stride + col);
             float v[V];
             t[r].get(v);
 #pragma unroll
             for (int i = 0; i < V; ++i) v[i] = there[r] ? v[i] * scale : 0.0f;
-            store_values<OUT>(y, v, dim - col, true);
+            w.template store_once<OUT>(at<OUT>(out.data, (p + r * per) * out.stride), v, dim);
         }
     }
 }
@@ -108,7 +137,7 @@ __device__ __forceinline__ void clear_rows(const ClearRows& c, uint32_t block, u
         if (c.named != nullptr && c.named[row] != 0u) continue;
         for (uint32_t s = 0; s < c.slices; ++s) {
             const uint32_t col = ((s << c.shift) + lane) * V;
-            if (col < c.dim) store_values<OUT>(at<OUT>(c.out.data, row * c.out.stride + col), zero, c.dim - col, true);
+            if (col < c.dim) Window<V>(col, c.dim).template store_once<OUT>(at<OUT>(c.out.data, row * c.out.stride), zero, c.dim);
         }
     }
 }
@@ -145,6 +174,11 @@ SortShape sort_shape(uint64_t tokens, uint64_t rows) {
     return s;
 }
 
+// Long runs are listed by the chunk they begin in (two neighbours are not both one's): with one counter for all, 400 of them wait for
+// each other (65536 positions of 64 values: the sums took 14.7 us instead of 11.5).
+constexpr uint32_t kJoinLists = 64, kJoinLine = 16;   // counters, and words between them
+inline uint64_t join_capacity(uint64_t chunks) { return (chunks / 2u + kJoinLists) / kJoinLists * kJoinLists; }
+
 struct SortArgs {
     TokenIds ids;
     uint64_t rows;
@@ -154,7 +188,7 @@ struct SortArgs {
     uint32_t* order_out;
     uint32_t* counts;         // [ranges][1 << bits]
     uint4* named;             // first pass, where rows are cleared: [rows] bytes, zeroed by the count and set by the scatter
-    uint32_t* join_count;     // first pass: cleared by the count
+    uint32_t* join_counts;    // cleared by the first launch
     uint64_t range;
     uint32_t ranges, bits, shift;
 };
@@ -187,7 +221,7 @@ template <bool WIDE>
 __global__ __launch_bounds__(kSortThreads) void sort_count_kernel(const SortArgs a, const ClearRows c) {
     __shared__ uint32_t s_count[kMaxDigits];
     const uint32_t digits = 1u << a.bits;
-    if (a.keys == nullptr && blockIdx.x == 0u && threadIdx.x == 0u) *a.join_count = 0u;
+    if (a.keys == nullptr && blockIdx.x == 0u && threadIdx.x < kJoinLists) a.join_counts[threadIdx.x * kJoinLine] = 0u;
     if (a.named != nullptr) {
         const uint64_t all = (a.rows + 15u) / 16u;
         for (uint64_t i = (uint64_t)blockIdx.x * kSortThreads + threadIdx.x; i < all; i += (uint64_t)gridDim.x * kSortThreads) a.named[i] = make_uint4(0u, 0u, 0u, 0u);
@@ -226,8 +260,9 @@ __global__ __launch_bounds__(kSortThreads) void sort_scatter_kernel(const SortAr
     }
     const uint32_t digits = 1u << a.bits, tid = threadIdx.x, lane = tid & 63u, wave = tid >> 6;
 
-    // the keys of a digit in all ranges, and in the earlier ones; the threads share the ranges out where digits are fewer
-    for (uint32_t d = tid; d < 2u * digits; d += kSortThreads) (d < digits ? s_next : s_wave[0])[d & (digits - 1u)] = 0u;
+    // the keys of a digit in all ranges (s_wave[0]), and in the earlier ones (s_next); the threads share the ranges out where digits are
+    // fewer.  (Counted here by every workgroup from all positions, without launches of their own: 66 -> 79 us for 16384 positions.)
+    for (uint32_t d = tid; d < digits; d += kSortThreads) s_next[d] = s_wave[0][d] = 0u;
     __syncthreads();
     {
         const uint32_t shares = digits < kSortThreads ? kSortThreads / digits : 1u;
@@ -331,7 +366,7 @@ __global__ __launch_bounds__(kOneThreads) void sort_one_kernel(const SortArgs a,
     }
     const uint32_t digits = 1u << a.bits, tid = threadIdx.x, lane = tid & 63u, wave = tid >> 6, count = (uint32_t)a.ids.count;
     const uint32_t items = (count + kOneThreads - 1u) / kOneThreads, first = wave * 64u * items + lane;   // a wave's keys are consecutive
-    if (tid == 0u) *a.join_count = 0u;
+    if (tid < kJoinLists) a.join_counts[tid * kJoinLine] = 0u;
     uint32_t key[kOneItems], from[kOneItems], rank[kOneItems];
 #pragma unroll
     for (uint32_t j = 0; j < kOneItems; ++j) {
@@ -436,7 +471,7 @@ __global__ __launch_bounds__(kThreads) void sum_few_kernel(const FewArgs a) {
             if (s_named[row - first] != 0u) continue;
             for (uint32_t s = 0; s < a.clear_slices; ++s) {
                 const uint32_t col = ((s << a.clear_shift) + (tid & ((1u << a.clear_shift) - 1u))) * VC;
-                if (col < a.dim) store_values<OUT>(at<OUT>(a.out.data, row * a.out.stride + col), zero, a.dim - col, true);
+                if (col < a.dim) Window<VC>(col, a.dim).template store_once<OUT>(at<OUT>(a.out.data, row * a.out.stride), zero, a.dim);
             }
         }
         return;
@@ -445,9 +480,10 @@ __global__ __launch_bounds__(kThreads) void sum_few_kernel(const FewArgs a) {
     const uint32_t p = blockIdx.x / a.slices, col = ((blockIdx.x - p * a.slices) * 64u + lane) * V;
     const uint32_t k = s_key[p];
     if (k >= rows) return;
-    const bool in = col < a.dim, whole = col + V <= a.dim;
+    const bool in = col < a.dim;
+    const Window<V> w(in ? col : 0u, a.dim);
     Pack<OUT, V> old;
-    void* y = at<OUT>(a.out.data, (uint64_t)k * a.out.stride + col);
+    void* y = at<OUT>(a.out.data, (uint64_t)k * a.out.stride);
     uint32_t found = 0;
     for (uint32_t i = 0; i < count; i += 64u) {
         const bool mine = i + lane < count && s_key[i + lane] == k;
@@ -457,10 +493,7 @@ __global__ __launch_bounds__(kThreads) void sum_few_kernel(const FewArgs a) {
         if (mine && wave == 0u) s_list[found + below] = i + lane;
         found += (uint32_t)__builtin_popcountll(all);
     }
-    if (a.accumulate && wave == 0u && in) {
-        if (whole) old.load(y);
-        else old.load_some(y, a.dim - col);
-    }
+    if (a.accumulate && wave == 0u && in) w.load(old, y, a.dim);
     __syncthreads();
     float sum[V] = {};
     for (uint32_t n = wave; n < found; n += kWaves * kFewSum) {   // the waves take the positions in turn
@@ -468,9 +501,7 @@ __global__ __launch_bounds__(kThreads) void sum_few_kernel(const FewArgs a) {
 #pragma unroll
         for (uint32_t j = 0; j < kFewSum; ++j) {
             if (!in || n + j * kWaves >= found) break;
-            const void* x = at<IN>(a.grad.data, (uint64_t)s_list[n + j * kWaves] * a.grad.stride + col);
-            if (whole) t[j].load(x);
-            else t[j].load_some(x, a.dim - col);
+            w.load(t[j], at<IN>(a.grad.data, (uint64_t)s_list[n + j * kWaves] * a.grad.stride), a.dim);
         }
 #pragma unroll
         for (uint32_t j = 0; j < kFewSum; ++j) {
@@ -489,20 +520,21 @@ __global__ __launch_bounds__(kThreads) void sum_few_kernel(const FewArgs a) {
         __syncthreads();
     }
     if (wave > 0u || !in) return;
-    for (uint32_t w = 1; w < min(found, kWaves); ++w) {
+    for (uint32_t n = 1; n < min(found, kWaves); ++n) {
 #pragma unroll
-        for (int l = 0; l < V; ++l) sum[l] += s_sum[w - 1u][lane][l];
+        for (int l = 0; l < V; ++l) sum[l] += s_sum[n - 1u][lane][l];
     }
     float v[V];
     if (a.accumulate) {
         old.get(v);
 #pragma unroll
         for (int l = 0; l < V; ++l) v[l] = __builtin_fmaf(a.scale, sum[l], v[l]);
+        w.template store_own<OUT>(y, v, a.dim);
     } else {
 #pragma unroll
         for (int l = 0; l < V; ++l) v[l] = a.scale * sum[l];
+        w.template store_once<OUT>(y, v, a.dim);
     }
-    store_values<OUT>(y, v, a.dim - col, !a.accumulate);
 }
 
 // ---- the sums ------------------------------------------------------------------------------------------
@@ -522,8 +554,8 @@ struct SumArgs {
     uint64_t count;                       // positions
     RowMatrix grad, out;
     float* partials;                      // [chunks][2][width]: of the long run that a chunk begins in, and of the one that begins in it
-    uint2* joins;                         // the long runs, in any order: the chunk that one begins in, and its partial sums
-    uint32_t* join_count;
+    uint2* joins;                         // the long runs, in kJoinLists lists: the chunk that one begins in, and its partial sums
+    uint32_t* join_counts;                // of the lists, kJoinLine apart
     uint32_t dim, width, chunk;           // width: dim, rounded up to 8
     uint32_t shift, slices;               // 1 << shift lanes hold a row, or one of its slices
     float scale;
@@ -531,52 +563,44 @@ struct SumArgs {
 };
 
 template <int OUT, int V>
-__device__ __forceinline__ void write_row(const SumArgs& a, uint32_t row, uint32_t col, const float (&sum)[V]) {
-    void* y = at<OUT>(a.out.data, (uint64_t)row * a.out.stride + col);
-    const uint32_t left = a.dim - col;
+__device__ __forceinline__ void write_row(const SumArgs& a, uint32_t row, const Window<V>& w, const float (&sum)[V]) {
+    void* y = at<OUT>(a.out.data, (uint64_t)row * a.out.stride);
     float v[V];
     if (a.accumulate) {
-        Pack<OUT, V> o;
-        if (left >= V) o.load(y);
-        else o.load_some(y, left);
-        o.get(v);
+        Pack<OUT, V> old;
+        w.load(old, y, a.dim);
+        old.get(v);
 #pragma unroll
         for (int i = 0; i < V; ++i) v[i] = __builtin_fmaf(a.scale, sum[i], v[i]);
+        w.template store_own<OUT>(y, v, a.dim);
     } else {
 #pragma unroll
         for (int i = 0; i < V; ++i) v[i] = a.scale * sum[i];
+        w.template store_once<OUT>(y, v, a.dim);
     }
-        store_values<OUT>(y, v, left, !a.accumulate);
 }
 
-
-// Puts the long run of key k, which begins in `chunk`, down for join_runs_kernel.  It ends with the last chunk that begins in it;
-// the search goes on here, where other workgroups have work to do meanwhile, by a wave at 64 chunks at a time, or by a lane.
-template <bool WAVE>
-__device__ __forceinline__ void list_run(const SumArgs& a, uint64_t chunk, uint32_t k, uint32_t lane) {
-    if (lane >= (WAVE ? 64u : 1u)) return;
-    const auto in = [&](uint64_t d) { return a.keys[(chunk + d) * a.chunk] == k; };
-    uint64_t low = 2, high = (a.count - 1u) / a.chunk - chunk + 1u;   // chunk + low - 1 begins in the run, chunk + high does not
-    if constexpr (WAVE) {
-        for (uint64_t step = 1; low < high; step = (high - low + 63u) / 64u) {   // the nearest first, which are all of most runs
+// Puts the long runs that begin in the wave's chunks down for join_runs_kernel: lanes with `begins`, each for a run of key k in `chunk`.
+// A run ends with the last chunk that begins in it; the search goes on here, where other workgroups have work to do meanwhile.
+// Call with every lane of the wave active.
+__device__ __forceinline__ void list_runs(const SumArgs& a, bool begins, uint32_t chunk, uint32_t k) {
+    const uint32_t lane = threadIdx.x & 63u;
+    for (uint64_t left = __builtin_amdgcn_ballot_w64(begins); left != 0u; left &= left - 1u) {
+        const int from = __builtin_ctzll(left);
+        const uint32_t c = (uint32_t)__builtin_amdgcn_readlane((int)chunk, from), key = (uint32_t)__builtin_amdgcn_readlane((int)k, from);
+        uint64_t low = 2, high = (a.count - 1u) / a.chunk - c + 1u;   // chunk c + low - 1 begins in the run, chunk c + high does not
+        for (uint64_t step = 1; low < high; step = (high - low + 63u) / 64u) {   // 64 at a time, the nearest first, which are all of most runs
             const uint64_t probe = low + lane * step;
-            const uint32_t seen = (uint32_t)__builtin_popcountll(__builtin_amdgcn_ballot_w64(probe < high && in(probe)));
+            const bool in = probe < high && a.keys[(c + probe) * a.chunk] == key;
+            const uint32_t seen = (uint32_t)__builtin_popcountll(__builtin_amdgcn_ballot_w64(in));
             if (seen < 64u) high = min(high, low + seen * step);
             if (seen > 0u) low += (seen - 1u) * step + 1u;
         }
-    } else {
-        for (uint64_t step = 1; low < high;) {                               // twice as far each time, then half as far
-            const uint64_t probe = min(low + step - 1u, high - 1u);
-            if (in(probe)) {
-                low = probe + 1u;
-                step *= 2u;
-            } else {
-                high = probe;
-                step = (high - low + 1u) / 2u;
-            }
+        if (lane == 0u) {
+            const uint32_t list = (c >> 1) % kJoinLists, n = atomicAdd(a.join_counts + list * kJoinLine, 1u);
+            a.joins[(uint64_t)n * kJoinLists + list] = make_uint2(c, (uint32_t)low);
         }
     }
-    if (lane == 0u) a.joins[atomicAdd(a.join_count, 1u)] = make_uint2((uint32_t)chunk, (uint32_t)low);
 }
 
 // The chunks of a workgroup, in one slice.  UNIFORM: a wave's lanes all belong to one chunk.
@@ -602,13 +626,12 @@ __device__ __forceinline__ void sum_chunks(const SumArgs& a, const uint64_t bloc
 
     const uint32_t start = team * a.chunk, end = start + a.chunk;
     uint32_t cur = key(start);
-    if (cur >= rows) return;                               // keys rise: no position from here on adds to a row
     const bool continues = key(start - 1u) == cur, head = continues && is_long(start, cur);
     const uint32_t last = key(end - 1u);
     const bool tail = last < rows && key(end) == last && is_long(end, last);
     const uint64_t chunk = block * per + team;
-    if (tail && !(continues && cur == last) && slice == 0u) list_run<UNIFORM>(a, chunk, last, lane);
-    if (col >= a.dim) return;
+    list_runs(a, slice == 0u && lane == 0u && tail && !(continues && cur == last), (uint32_t)chunk, last);
+    if (cur >= rows || col >= a.dim) return;               // keys rise: no position from here on adds to a row
     uint32_t i = start, stop = end;
     if (continues && !head) {                              // the chunk before this one adds it up
         while (i < end && key(i) == cur) ++i;
@@ -620,26 +643,24 @@ __device__ __forceinline__ void sum_chunks(const SumArgs& a, const uint64_t bloc
     } else if (!tail) {
         while (key(stop) == last) ++stop;                  // less than a chunk: the run is not long
     }
+    const Window<V> w(col, a.dim);
     float sum[V] = {};
     uint32_t run = head ? 0u : ~0u;                        // the slot of the run's partial sum; ~0u: the run is whole
     const auto finish = [&] {
         if (run == ~0u) {
-            write_row<OUT, V>(a, cur, col, sum);
+            write_row<OUT, V>(a, cur, w, sum);
             return;
         }
         Pack<kF32, V> o;
         o.set(sum);
-        o.store(a.partials + (2u * chunk + run) * a.width + col);   // col and width are whole numbers of V
+        o.store(a.partials + (2u * chunk + run) * a.width + w.at);
     };
-    const bool whole = col + V <= a.dim;
     for (; i < stop; i += kRows) {
         Pack<IN, V> t[kRows];
 #pragma unroll
         for (uint32_t j = 0; j < kRows; ++j) {             // past the end: the last row again
             const uint32_t from = scalar(s_order[min(i + j, stop - 1u)]);
-            const void* x = at<IN>(a.grad.data, (uint64_t)from * a.grad.stride + col);
-            if (whole) t[j].load_once(x);
-            else t[j].load_some(x, a.dim - col);
+            w.load_once(t[j], at<IN>(a.grad.data, (uint64_t)from * a.grad.stride), a.dim);
         }
 #pragma unroll
         for (uint32_t j = 0; j < kRows; ++j) {
@@ -672,30 +693,32 @@ __global__ __launch_bounds__(kThreads) void sum_runs_kernel(const SumArgs a) {
     }
 }
 
-// The partial sums of a long run: the waves take them in turn, and add up theirs in order.
-constexpr uint32_t kJoinWaves = 8, kJoinThreads = 64u * kJoinWaves, kJoinBlocks = 256;
+// The partial sums of a long run: `1 << join_shift` lanes hold one (or a slice of one), four values each; they take them in turn, add up
+// theirs in order, and one of them adds up all.
+constexpr uint32_t kJoinThreads = 512, kJoinBlocks = 512;
 template <int OUT>
-__global__ __launch_bounds__(kJoinThreads) void join_runs_kernel(const SumArgs a) {
-    __shared__ float s_sum[kJoinWaves][64][4];
-    const uint32_t lane = threadIdx.x & 63u, wave = threadIdx.x >> 6, col = (blockIdx.y * 64u + lane) * 4u;
-    const uint32_t joins = *a.join_count;
-    for (uint32_t n = blockIdx.x; n < joins; n += gridDim.x) {
-        const uint2 join = a.joins[n];
-        const uint64_t c = join.x, parts = join.y;                    // slot 1 of c, slot 0 of c + 1 .. c + parts - 1
+__global__ __launch_bounds__(kJoinThreads) void join_runs_kernel(const SumArgs a, const uint32_t shift) {
+    __shared__ float s_sum[kJoinThreads][4];
+    const uint32_t teams = kJoinThreads >> shift, team = threadIdx.x >> shift, col = ((blockIdx.y << shift) + (threadIdx.x & ((1u << shift) - 1u))) * 4u;
+    const uint32_t list = blockIdx.x % kJoinLists, joins = a.join_counts[list * kJoinLine];
+    for (uint32_t n = blockIdx.x / kJoinLists; n < joins; n += gridDim.x / kJoinLists) {
+        const uint2 join = a.joins[(uint64_t)n * kJoinLists + list];
+        const uint64_t c = join.x;
+        const uint32_t parts = join.y;                                // slot 1 of c, slot 0 of c + 1 .. c + parts - 1
         const uint32_t k = a.keys[(c + 1u) * a.chunk];
         float sum[4] = {};
         if (col < a.width) {
             constexpr uint32_t kAhead = 8;
-            for (uint64_t p = wave; p < parts; p += kAhead * kJoinWaves) {
+            for (uint32_t p = team; p < parts; p += kAhead * teams) {
                 Pack<kF32, 4> t[kAhead];
 #pragma unroll
                 for (uint32_t j = 0; j < kAhead; ++j) {
-                    const uint64_t part = min(p + j * kJoinWaves, parts - 1u);
+                    const uint32_t part = min(p + j * teams, parts - 1u);
                     t[j].load(a.partials + (2u * (c + part) + (part == 0u ? 1u : 0u)) * a.width + col);
                 }
 #pragma unroll
                 for (uint32_t j = 0; j < kAhead; ++j) {
-                    if (p + j * kJoinWaves >= parts) break;
+                    if (p + j * teams >= parts) break;
                     float v[4];
                     t[j].get(v);
 #pragma unroll
@@ -705,15 +728,23 @@ __global__ __launch_bounds__(kJoinThreads) void join_runs_kernel(const SumArgs a
         }
         __syncthreads();                                              // the run before this one has been added up
 #pragma unroll
-        for (int l = 0; l < 4; ++l) s_sum[wave][lane][l] = sum[l];
+        for (int l = 0; l < 4; ++l) s_sum[threadIdx.x][l] = sum[l];
         __syncthreads();
-        if (wave == 0u && col < a.dim) {
+        if (team == 0u && col < a.dim) {
+            for (uint32_t other = 1; other < min(teams, parts); ++other) {
 #pragma unroll
-            for (uint32_t w = 1; w < kJoinWaves; ++w) {
-#pragma unroll
-                for (int l = 0; l < 4; ++l) sum[l] += s_sum[w][lane][l];
+                for (int l = 0; l < 4; ++l) sum[l] += s_sum[(other << shift) + threadIdx.x][l];
             }
-            write_row<OUT, 4>(a, k, col, sum);
+            // from four values at `col` to a window of the row
+            const Window<4> w(col, a.dim);
+            void* y = at<OUT>(a.out.data, (uint64_t)k * a.out.stride);
+#pragma unroll
+            for (int l = 0; l < 4; ++l) {
+                if (w.skip != 0u || w.narrow) {
+                    if (col + l < a.dim) store_one<OUT>(y, col + l, a.accumulate ? __builtin_fmaf(a.scale, sum[l], load_one<OUT>(y, col + l)) : a.scale * sum[l]);
+                }
+            }
+            if (w.skip == 0u && !w.narrow) write_row<OUT, 4>(a, k, w, sum);
         }
     }
 }
@@ -733,18 +764,24 @@ RowShape row_shape(uint64_t rows, uint32_t dim, uint32_t v) {
     return s;
 }
 
-// Positions of a chunk: enough chunks to fill the GPU, as long as that allows (a long run leaves a partial sum in every chunk),
-// and no more than LDS holds of a workgroup's.  The same for all types, which the size of the workspace does not depend on.
+// Positions of a chunk: as many as leave 4096 waves, and as many as leave 1024 where there are more than 2048 chunks, whose partial sums
+// a long run's join waits for; no more than LDS holds of a workgroup's.  (65536 positions of 435 values, 8 and 32: 72 and 68 us; of 64
+// values, which leave 256 waves with chunks of 32: 46 and 53; 131072 of 4096 values, 16, 32 and 64: 698, 654 and 632.)  The same for all
+// types, which the size of the workspace does not depend on.
 uint32_t chunk_of(uint64_t tokens, uint32_t dim) {
-    const uint32_t per = kThreads >> row_shape(1, dim, 8u).shift;   // most chunks of a workgroup: 8 values a lane
-    const uint64_t waves = tokens * ((dim + 511u) / 512u);
+    const RowShape g = row_shape(1, dim, 8u);
+    const uint32_t per = kThreads >> g.shift;                       // most chunks of a workgroup: 8 values a lane
+    const uint64_t waves = tokens * g.slices * (kThreads / 64u) / per;   // of chunks of one position
     uint32_t chunk = kMostPositions / kThreads;
-    while (chunk < kMostChunk && per * chunk < kMostPositions && waves / (2u * chunk) >= 4096u) chunk *= 2u;
+    while (chunk < kMostChunk && per * chunk < kMostPositions &&
+           (waves / (2u * chunk) >= 4096u || (waves / (2u * chunk) >= 1024u && tokens / chunk > 2048u))) {
+        chunk *= 2u;
+    }
     return chunk;
 }
 
 struct GradWorkspace {
-    uint32_t *keys[2], *order[2], *counts, *named, *join_count;
+    uint32_t *keys[2], *order[2], *counts, *named, *join_counts;
     uint2* joins;
     float* partials;
     size_t bytes;
@@ -767,8 +804,8 @@ GradWorkspace grad_workspace(void* base, uint64_t tokens, uint32_t dim, uint64_t
     }
     w.counts = take((uint64_t)s.ranges << s.bits);
     const uint64_t chunks = (tokens + chunk_of(tokens, dim) - 1u) / chunk_of(tokens, dim);
-    w.join_count = take(1);
-    w.joins = reinterpret_cast<uint2*>(take(chunks + 2u));        // of two neighbours, one at most: a long run covers the chunk behind the one it begins in
+    w.join_counts = take(kJoinLists * kJoinLine);
+    w.joins = reinterpret_cast<uint2*>(take(2u * join_capacity(chunks)));
     w.partials = reinterpret_cast<float*>(take(chunks * 2u * ((dim + 7u) & ~7u)));
     return w;
 }
@@ -838,7 +875,7 @@ hipError_t launch_embedding_grad(const RowMatrix& grad_out, const TokenIds& ids,
     a.ranges = s.ranges;
     a.bits = s.bits;
     a.named = accumulate ? nullptr : reinterpret_cast<uint4*>(w.named);
-    a.join_count = w.join_count;
+    a.join_counts = w.join_counts;
     // The rows to clear are shared out over the launches of the sort: to each but the last as much as takes about as long as the
     // launch does without, to the last all that is left.  Rows that are cleared before the names are known are cleared for
     // nothing where they are named, which the last rows of a vocabulary seldom are: from the last row on.
@@ -886,7 +923,7 @@ hipError_t launch_embedding_grad(const RowMatrix& grad_out, const TokenIds& ids,
     b.out = table_grad;
     b.partials = w.partials;
     b.joins = w.joins;
-    b.join_count = w.join_count;
+    b.join_counts = w.join_counts;
     b.dim = dim;
     b.width = (dim + 7u) & ~7u;
     b.chunk = chunk_of(ids.count, dim);
@@ -905,7 +942,10 @@ hipError_t launch_embedding_grad(const RowMatrix& grad_out, const TokenIds& ids,
     e = hipGetLastError();
     if (e != hipSuccess || chunks < 3u) return e;   // a long run touches three chunks
     with_dtype(table_grad.dtype, [&](auto o) {
-        hipLaunchKernelGGL((join_runs_kernel<o>), dim3((uint32_t)std::min<uint64_t>(chunks / 2u, kJoinBlocks), (b.width + 255u) / 256u), dim3(kJoinThreads), 0, stream, b);
+        uint32_t shift = 0;
+        while (shift < 6u && (4u << shift) < dim) ++shift;
+        const uint32_t slice = 4u << shift;
+        hipLaunchKernelGGL((join_runs_kernel<o>), dim3((uint32_t)std::min<uint64_t>(join_capacity(chunks), kJoinBlocks), (dim + slice - 1u) / slice), dim3(kJoinThreads), 0, stream, b, shift);
     });
     return hipGetLastError();
 }
