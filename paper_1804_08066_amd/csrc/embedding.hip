@@ -151,8 +151,10 @@ __global__ __launch_bounds__(kThreads) void clear_rows_kernel(const ClearRows c)
 // Least significant digit first.  Every workgroup owns a range of the positions; a pass counts each range's digits, and the
 // scatter adds up the counts before its own (of smaller digits, and of equal ones in earlier ranges) by itself.  The sort of a
 // batch is a handful of workgroups that wait for memory, so the launches clear rows of the table beside it.
-constexpr uint32_t kSortThreads = 512, kSortWaves = kSortThreads / 64u, kSortItems = 4, kSortTile = kSortThreads * kSortItems;
-constexpr uint32_t kMaxRanges = 128;     // every workgroup reads all ranges' counts: a few, of any length
+constexpr uint32_t kSortThreads = 512, kSortWaves = kSortThreads / 64u, kSortItems = 1, kSortTile = kSortThreads * kSortItems;
+// Every workgroup reads all ranges' counts: a range holds up to four tiles before there are more than kRanges of them.  (16384 positions
+// of 1024 values in tiles of 512, 1024, 2048 and 4096: 44.5, 46.5, 51 and 60 us.)
+constexpr uint32_t kRanges = 64, kMaxRanges = 256, kRangeTiles = 4;
 constexpr uint32_t kMaxDigitBits = 10, kMaxDigits = 1u << kMaxDigitBits;
 
 constexpr uint64_t kClearBeside = 50000000;   // bytes
@@ -168,7 +170,8 @@ SortShape sort_shape(uint64_t tokens, uint64_t rows) {
     while ((rows >> all) != 0u) ++all;    // keys are 0 .. rows
     s.passes = (all + kMaxDigitBits - 1u) / kMaxDigitBits;
     s.bits = (all + s.passes - 1u) / s.passes;
-    const uint64_t tiles = (tokens + kSortTile - 1u) / kSortTile, each = (tiles + kMaxRanges - 1u) / kMaxRanges;
+    const uint64_t tiles = (tokens + kSortTile - 1u) / kSortTile;
+    const uint64_t most = std::min<uint64_t>(kMaxRanges, std::max<uint64_t>(kRanges, tiles / kRangeTiles)), each = (tiles + most - 1u) / most;
     s.range = each * kSortTile;
     s.ranges = (uint32_t)((tokens + s.range - 1u) / s.range);
     return s;
@@ -260,6 +263,19 @@ __global__ __launch_bounds__(kSortThreads) void sort_scatter_kernel(const SortAr
     }
     const uint32_t digits = 1u << a.bits, tid = threadIdx.x, lane = tid & 63u, wave = tid >> 6;
 
+    const uint64_t first = (uint64_t)blockIdx.x * a.range, end = min(first + a.range, a.ids.count);
+    const uint32_t mine = wave * (64u * kSortItems) + lane;   // a wave's keys are consecutive, 64 at a time
+    uint32_t key[kSortItems], from[kSortItems];
+    const auto load = [&](uint64_t tile) {
+#pragma unroll
+        for (uint32_t j = 0; j < kSortItems; ++j) {
+            const uint64_t i = tile + mine + j * 64u;
+            key[j] = i < end ? sort_key<WIDE>(a, i) : 0u;
+            from[j] = i < end && a.order != nullptr ? a.order[i] : (uint32_t)i;
+        }
+    };
+    load(first);   // on their way while the counts are added up
+
     // the keys of a digit in all ranges (s_wave[0]), and in the earlier ones (s_next); the threads share the ranges out where digits are
     // fewer.  (Counted here by every workgroup from all positions, without launches of their own: 66 -> 79 us for 16384 positions.)
     for (uint32_t d = tid; d < digits; d += kSortThreads) s_next[d] = s_wave[0][d] = 0u;
@@ -290,9 +306,9 @@ __global__ __launch_bounds__(kSortThreads) void sort_scatter_kernel(const SortAr
     __syncthreads();
     // the keys of smaller digits: every thread adds up consecutive digits
     const uint32_t per = (digits + kSortThreads - 1u) / kSortThreads;   // 1 or 2
-    uint32_t mine = 0;
-    for (uint32_t j = 0; j < per; ++j) mine += tid * per + j < digits ? s_wave[0][tid * per + j] : 0u;
-    uint32_t upto = mine;
+    uint32_t own = 0;
+    for (uint32_t j = 0; j < per; ++j) own += tid * per + j < digits ? s_wave[0][tid * per + j] : 0u;
+    uint32_t upto = own;
 #pragma unroll
     for (uint32_t m = 1; m < 64u; m <<= 1) {
         const uint32_t other = __shfl_up(upto, m, 64);
@@ -300,7 +316,7 @@ __global__ __launch_bounds__(kSortThreads) void sort_scatter_kernel(const SortAr
     }
     if (lane == 63u) s_total[wave] = upto;
     __syncthreads();
-    uint32_t at = upto - mine;
+    uint32_t at = upto - own;
     for (uint32_t w = 0; w < wave; ++w) at += s_total[w];
     for (uint32_t j = 0; j < per; ++j) {
         const uint32_t d = tid * per + j;
@@ -309,23 +325,14 @@ __global__ __launch_bounds__(kSortThreads) void sort_scatter_kernel(const SortAr
         at += s_wave[0][d];
     }
 
-    const uint64_t first = (uint64_t)blockIdx.x * a.range, end = min(first + a.range, a.ids.count);
     for (uint64_t tile = first; tile < end; tile += kSortTile) {
-        uint32_t key[kSortItems], from[kSortItems], rank[kSortItems];
-        bool valid[kSortItems];
-#pragma unroll
-        for (uint32_t j = 0; j < kSortItems; ++j) {   // a wave's keys are consecutive, in this order
-            const uint64_t i = tile + (uint64_t)wave * (64u * kSortItems) + j * 64u + lane;
-            valid[j] = i < end;
-            key[j] = valid[j] ? sort_key<WIDE>(a, i) : 0u;
-            from[j] = valid[j] && a.order != nullptr ? a.order[i] : (uint32_t)i;
-        }
+        uint32_t rank[kSortItems];
         __syncthreads();
         for (uint32_t d = lane; d < digits; d += 64u) s_wave[wave][d] = 0u;
         __builtin_amdgcn_wave_barrier();
 #pragma unroll
         for (uint32_t j = 0; j < kSortItems; ++j) {
-            rank[j] = rank_in_wave(s_wave[wave], (key[j] >> a.shift) & (digits - 1u), a.bits, valid[j]);
+            rank[j] = rank_in_wave(s_wave[wave], (key[j] >> a.shift) & (digits - 1u), a.bits, tile + mine + j * 64u < end);
         }
         __syncthreads();
         for (uint32_t d = tid; d < digits; d += kSortThreads) {
@@ -341,12 +348,13 @@ __global__ __launch_bounds__(kSortThreads) void sort_scatter_kernel(const SortAr
         __syncthreads();
 #pragma unroll
         for (uint32_t j = 0; j < kSortItems; ++j) {
-            if (!valid[j]) continue;
+            if (tile + mine + j * 64u >= end) continue;
             const uint32_t to = s_wave[wave][(key[j] >> a.shift) & (digits - 1u)] + rank[j];
             a.keys_out[to] = key[j];
             a.order_out[to] = from[j];
             if (a.named != nullptr && key[j] < a.rows) reinterpret_cast<uint8_t*>(a.named)[key[j]] = 1u;
         }
+        load(tile + kSortTile);
     }
 }
 
