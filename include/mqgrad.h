@@ -425,7 +425,8 @@ typedef struct {
  *   workspace   device, mqg_global_norm_workspace_bytes(count) bytes of scratch memory, 8-byte aligned; contents on
  *               entry are of no interest, contents on return are unspecified.  Calls that share a workspace must not overlap.
  *   norm_out    device, one double, 8-byte aligned, overwritten (0 where there are no values).
- * Errors: MQG_EINVAL (NULL pointer, unknown type, too many tensors or over 8 * 10^12 values), MQG_EALIGN, MQG_ELAUNCH. */
+ * Errors: MQG_EINVAL (NULL pointer, unknown type, too many tensors or over 8 * 10^12 values, workspace or norm_out over a tensor or
+ * over each other), MQG_EALIGN, MQG_ELAUNCH. */
 size_t mqg_global_norm_workspace_bytes(uint32_t count);
 mqg_status mqg_global_norm(const mqg_clip_item* items, uint32_t count, void* workspace, double* norm_out, void* stream);
 
@@ -439,7 +440,7 @@ mqg_status mqg_global_norm(const mqg_clip_item* items, uint32_t count, void* wor
 mqg_status mqg_clip_by_norm(const mqg_clip_item* items, uint32_t count, const double* norm, double max_norm, void* stream);
 
 /* mqg_global_norm, then mqg_clip_by_norm with that norm.  Arguments and errors as above; neither workspace nor norm_out may
- * lie in an output. */
+ * lie over a tensor or an output. */
 mqg_status mqg_clip_global_norm(const mqg_clip_item* items, uint32_t count, double max_norm, void* workspace, double* norm_out,
                                 void* stream);
 

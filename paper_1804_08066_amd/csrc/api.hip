@@ -162,6 +162,10 @@ struct Span {
     bool written;
 };
 bool overlap(const Span& a, const Span& b) { return a.at < b.end && b.at < a.end; }
+Span span_of(const void* p, uint64_t bytes, uint32_t item = 0u, bool written = false) {
+    const uintptr_t at = reinterpret_cast<uintptr_t>(p);
+    return {at, at + bytes, item, written};
+}
 
 // Whether a written span of `spans` lies over any other, an item's own two being the same span excepted.  Sorts them.
 bool writes_collide(Span* spans, uint32_t count) {
@@ -202,7 +206,8 @@ mqg_status norm_items(const mqg_clip_item* items, uint32_t count) {
     }
     return MQG_OK;
 }
-// the outputs of a clipping call; norm_items first.  scratch, scratch_bytes: what the call writes besides
+// the outputs of a clipping call; norm_items first.  scratch, scratch_bytes: what the call writes besides, together with *norm; none where
+// the norm is given
 mqg_status clip_items(const mqg_clip_item* items, uint32_t count, double max_norm, const void* norm, const void* scratch, size_t scratch_bytes) {
     if (!(max_norm >= 0.0)) return MQG_EINVAL;
     for (uint32_t i = 0; i < count; ++i) {
@@ -218,21 +223,17 @@ mqg_status clip_items(const mqg_clip_item* items, uint32_t count, double max_nor
     if (spans == nullptr) return MQG_ELAUNCH;
     uint32_t used = 0;
     bool bad = false;
-    const auto span = [](const void* p, uint64_t bytes, uint32_t item, bool written) {
-        const uintptr_t at = reinterpret_cast<uintptr_t>(p);
-        return Span{at, at + bytes, item, written};
-    };
     for (uint32_t i = 0; i < count; ++i) {
         const mqg_clip_item& it = items[i];
         if (it.n == 0) continue;
-        const Span in = span(it.data, it.n * size_of(it.dtype), i + 1u, false), out = span(it.out, it.n * size_of(it.out_dtype), i + 1u, true);
+        const Span in = span_of(it.data, it.n * size_of(it.dtype), i + 1u, false), out = span_of(it.out, it.n * size_of(it.out_dtype), i + 1u, true);
         const bool in_place = it.data == it.out && it.dtype == it.out_dtype;
         bad = bad || (!in_place && overlap(in, out));
         if (!in_place) spans[used++] = in;
         spans[used++] = out;
     }
-    spans[used++] = span(norm, sizeof(double), count + 1u, false);
-    if (scratch_bytes != 0) spans[used++] = span(scratch, scratch_bytes, count + 2u, false);
+    spans[used++] = span_of(norm, sizeof(double), count + 1u, scratch != nullptr);
+    if (scratch != nullptr) spans[used++] = span_of(scratch, scratch_bytes, count + 2u, true);
     bad = bad || writes_collide(spans, used);
     if (spans != few) delete[] spans;
     return bad ? MQG_EINVAL : MQG_OK;
@@ -240,8 +241,7 @@ mqg_status clip_items(const mqg_clip_item* items, uint32_t count, double max_nor
 
 // a matrix's memory, from its first value to behind its last
 Span span_of(const mqg_rows& m, uint32_t dim) {
-    const uintptr_t at = reinterpret_cast<uintptr_t>(m.data);
-    return {at, m.rows == 0 ? at : at + ((m.rows - 1u) * m.stride + dim) * size_of(m.dtype), 0, false};
+    return span_of(m.data, m.rows == 0 ? 0u : ((m.rows - 1u) * m.stride + dim) * size_of(m.dtype));
 }
 mqg_status rows_args(const mqg_rows* m, uint64_t most_rows, uint32_t dim, bool written, mqg::RowMatrix& out) {
     if (m == nullptr || size_of(m->dtype) == 0u || m->rows > most_rows) return MQG_EINVAL;
@@ -260,10 +260,7 @@ mqg_status tokens_args(const mqg_tokens* t, mqg::TokenIds& out) {
     out = mqg::TokenIds{t->ids, t->count, t->type == MQG_INDEX64 ? 1 : 0, t->first_row, t->padding_id};
     return MQG_OK;
 }
-Span span_of(const mqg_tokens& t) {
-    const uintptr_t at = reinterpret_cast<uintptr_t>(t.ids);
-    return {at, at + t.count * (t.type == MQG_INDEX64 ? 8u : 4u), 0, false};
-}
+Span span_of(const mqg_tokens& t) { return span_of(t.ids, t.count * (t.type == MQG_INDEX64 ? 8u : 4u)); }
 
 }  // namespace
 
@@ -750,6 +747,12 @@ mqg_status mqg_global_norm(const mqg_clip_item* items, uint32_t count, void* wor
     if (st != MQG_OK) return st;
     if (norm_out == nullptr || (count > 0u && workspace == nullptr)) return MQG_EINVAL;
     if (misaligned8(norm_out) || misaligned8(workspace)) return MQG_EALIGN;
+    const Span out = span_of(norm_out, sizeof(double)), scratch = span_of(workspace, mqg_global_norm_workspace_bytes(count));
+    if (overlap(out, scratch)) return MQG_EINVAL;
+    for (uint32_t i = 0; i < count; ++i) {
+        const Span in = span_of(items[i].data, items[i].n * size_of(items[i].dtype));
+        if (overlap(in, out) || overlap(in, scratch)) return MQG_EINVAL;
+    }
     const hipError_t err = mqg::launch_global_norm(items, count, static_cast<double*>(workspace), norm_out, static_cast<hipStream_t>(stream));
     return err == hipSuccess ? MQG_OK : MQG_ELAUNCH;
 }
@@ -809,8 +812,7 @@ mqg_status mqg_embedding_grad(const mqg_rows* grad_out, const mqg_tokens* tokens
     const size_t need = mqg::embedding_grad_workspace(ids.count, dim, o.rows);
     if (need != 0 && workspace == nullptr) return MQG_EINVAL;
     if (misaligned(workspace, 16u)) return MQG_EALIGN;
-    const uintptr_t ws = reinterpret_cast<uintptr_t>(workspace);
-    const Span out = span_of(*table_grad, dim), in = span_of(*grad_out, dim), at = span_of(*tokens), scratch = {ws, ws + need, 0, false};
+    const Span out = span_of(*table_grad, dim), in = span_of(*grad_out, dim), at = span_of(*tokens), scratch = span_of(workspace, need);
     if (overlap(out, in) || overlap(out, at) || overlap(out, scratch) || overlap(in, scratch) || overlap(at, scratch)) return MQG_EINVAL;
     const hipError_t err = mqg::launch_embedding_grad(g, ids, dim, scale, o, accumulate != 0, workspace, static_cast<hipStream_t>(stream));
     return err == hipSuccess ? MQG_OK : MQG_ELAUNCH;

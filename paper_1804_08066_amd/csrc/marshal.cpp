@@ -577,7 +577,9 @@ mqg_rows rows_of(PyObject* o, const Device& d, uint64_t* dim) {
 mqg_tokens tokens_of(PyObject* o, const Device& d, PyObject* first_row, PyObject* padding) {
     const at::Tensor& t = values(o, d);
     if (t.scalar_type() != at::kInt && t.scalar_type() != at::kLong) throw Reject{};
-    return mqg_tokens{t.data_ptr(), (uint64_t)t.numel(), t.scalar_type() == at::kLong ? MQG_INDEX64 : MQG_INDEX32, integer(first_row),
+    const int64_t first = integer(first_row);
+    if (first < 0 || first > (int64_t)1 << 62) throw Reject{};
+    return mqg_tokens{t.data_ptr(), (uint64_t)t.numel(), t.scalar_type() == at::kLong ? MQG_INDEX64 : MQG_INDEX32, first,
                       padding == Py_None ? INT64_MIN : integer(padding)};
 }
 // embedding(table, ids, scale, first_row, out, stream) -> status

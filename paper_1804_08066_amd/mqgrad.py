@@ -806,12 +806,16 @@ def _one_device(tensors):
             raise ValueError("all tensors must be on the current device, cuda:%d" % device)
 
 
-def _scratch(need, stream, device):
-    """A workspace of a call's own, which the stream keeps until its work is done."""
-    workspace = torch.empty(need, dtype=torch.uint8, device=device)
-    if stream is not None and workspace.is_cuda:
-        workspace.record_stream(stream)
-    return workspace
+def _empty(shape, dtype, device, stream):
+    """A buffer of a call's own.  On a stream that is not the current one it comes from that stream's memory, where nothing that the
+    current stream has yet to do can reach it, and outlives what the current stream does with it."""
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    with torch.cuda.stream(stream):
+        t = torch.empty(shape, dtype=dtype, device=device)
+    if t.is_cuda:
+        t.record_stream(torch.cuda.current_stream())
+    return t
 
 
 def _check_scratch(workspace, need):
@@ -860,9 +864,9 @@ def _norm_buffers(tensors, workspace, norm_out, stream):
     if workspace is None or norm_out is None:
         dev = tensors[0].device if len(tensors) else "cuda"
         if workspace is None:
-            workspace = _scratch(mqg_global_norm_workspace_bytes(len(tensors)), stream, dev)
+            workspace = _empty(mqg_global_norm_workspace_bytes(len(tensors)), torch.uint8, dev, stream)
         if norm_out is None:
-            norm_out = torch.empty(1, dtype=torch.float64, device=dev)
+            norm_out = _empty(1, torch.float64, dev, stream)
     return workspace, norm_out
 
 
@@ -956,7 +960,7 @@ def mqg_embedding(table, ids, scale=1.0, first_row=0, out=None, stream=None):
     t, dim = _rows(table, "table")
     tokens = _tokens(ids, first_row, _NO_PADDING)
     if out is None:
-        out = torch.empty(*ids.shape, dim, dtype=table.dtype, device=table.device)
+        out = _empty((*ids.shape, dim), table.dtype, table.device, stream)
     o, out_dim = _rows(out, "out")
     if out_dim != dim or o.rows != tokens.count:
         raise ValueError("out must hold one row of the table for every token")
@@ -990,13 +994,13 @@ def mqg_embedding_grad(grad_out, ids, rows, scale=1.0, first_row=0, padding_id=N
     if out is None:
         if accumulate:
             raise ValueError("accumulate adds to out, which must be given")
-        out = torch.empty(rows, dim, dtype=grad_out.dtype, device=grad_out.device)
+        out = _empty((rows, dim), grad_out.dtype, grad_out.device, stream)
     o, out_dim = _rows(out, "out")
     if out_dim != dim or o.rows != rows:
         raise ValueError("out must have %d rows of grad_out's width" % rows)
     need = mqg_embedding_grad_workspace_bytes(tokens.count, dim, rows)
     if workspace is None:
-        workspace = _scratch(need, stream, out.device)
+        workspace = _empty(need, torch.uint8, out.device, stream)
     _check_scratch(workspace, need)
     _one_device([grad_out, ids, out, workspace])
     st = _lib.mqg_embedding_grad(C.byref(g), C.byref(tokens), dim, scale, C.byref(o), 1 if accumulate else 0, workspace.data_ptr(),

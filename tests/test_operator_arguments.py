@@ -62,7 +62,10 @@ def test_norm_and_its_places_are_checked():
     assert norm(good, workspace=None) == mq.MQG_EINVAL
     assert norm(good, out=None) == mq.MQG_EINVAL
     assert norm(good, out=B + 4) == mq.MQG_EALIGN
-    assert norm(good, workspace=A + 4) == mq.MQG_EALIGN
+    assert norm(good, workspace=0x40004) == mq.MQG_EALIGN
+    assert norm(good, workspace=A - 64) == mq.MQG_EINVAL                 # over the tensor
+    assert norm(good, workspace=0x40000, out=A + 32) == mq.MQG_EINVAL
+    assert norm(good, workspace=B - 64) == mq.MQG_EINVAL                 # over the norm
     clip = items((A, B, 10, F32, F32))
     assert by_norm(clip, at=None) == mq.MQG_EINVAL
     assert by_norm(clip, at=0x8004) == mq.MQG_EALIGN
@@ -75,7 +78,7 @@ def test_norm_and_its_places_are_checked():
         assert call(items((A, B + 1, 10, F32, BF16))) == mq.MQG_EALIGN
     assert both(clip, workspace=None) == mq.MQG_EINVAL
     assert both(clip, out=None) == mq.MQG_EINVAL
-    assert both(clip, workspace=A + 4) == mq.MQG_EALIGN
+    assert both(clip, workspace=0x40004) == mq.MQG_EALIGN
     assert by_norm(items((A, B, 0, F32, F32))) == mq.MQG_OK       # nothing to do
     assert by_norm(items(), 0) == mq.MQG_OK
 
@@ -94,6 +97,8 @@ def test_outputs_over_other_memory_are_refused(call):
     assert call(items(*many, (A + 512 * 17 + 508, 0x40000, 1, F32, F32))) == mq.MQG_EINVAL
     if call is both:
         assert both(items((A, B, n, F32, F32)), workspace=B - 64) == mq.MQG_EINVAL
+        assert both(items((A, B, n, F32, F32)), workspace=A - 64) == mq.MQG_EINVAL   # over an input
+        assert both(items((A, B, n, F32, F32)), out=A + 8) == mq.MQG_EINVAL
 
 
 def test_the_check_of_outputs_agrees_with_all_pairs():
