@@ -81,8 +81,8 @@ __device__ __forceinline__ double workgroup_sum(double acc) {
 }
 
 // The workgroups take pieces in turn: a partial sum of each.
-template <bool ONCE>
-__global__ __launch_bounds__(kThreads) void norm_partial_kernel(const NormTable b, double* __restrict__ partials) {
+template <bool ONCE, class Table>
+__global__ __launch_bounds__(kThreads) void norm_partial_kernel(const Table b, double* __restrict__ partials) {
     double acc = 0.0;
     for (uint32_t piece = blockIdx.x; piece < b.pieces; piece += gridDim.x) {
         const uint32_t k = tensor_of_piece(b.start, b.count, piece);
@@ -117,14 +117,16 @@ __global__ __launch_bounds__(kThreads) void norm_finish_kernel(const double* __r
 // a norm that is not a number makes the factor one too: nothing hides it
 __device__ __forceinline__ float clip_factor(double norm, double max_norm) { return norm <= max_norm ? 1.0f : (float)(max_norm / norm); }
 
-template <int IN, int OUT>
-__device__ __forceinline__ void clip_piece(const void* x, void* y, const uint32_t count, const float c) {
+// factor() is asked for when the values are on their way
+template <int IN, int OUT, class F>
+__device__ __forceinline__ void clip_piece(const void* x, void* y, const uint32_t count, F factor) {
     constexpr int V = IN == kF32 || OUT == kF32 ? 4 : 8;
     constexpr uint32_t kRow = kThreads * V, kRows = kPiece / kRow;
     if (count == kPiece) {
         Pack<IN, V> t[kRows];
 #pragma unroll
         for (uint32_t r = 0; r < kRows; ++r) t[r].load_once(at<IN>(x, r * kRow + threadIdx.x * V));
+        const float c = factor();
 #pragma unroll
         for (uint32_t r = 0; r < kRows; ++r) {
             float v[V];
@@ -137,22 +139,27 @@ __device__ __forceinline__ void clip_piece(const void* x, void* y, const uint32_
         }
         return;
     }
+    const float c = factor();
     for (uint32_t i = threadIdx.x; i < count; i += kThreads) store_one<OUT>(y, i, load_one<IN>(x, i) * c);
 }
 
 // A workgroup for every piece.  (2048 that take pieces in turn: 1745 us instead of 1677 for 1.2 G values in pieces of 8192.)
-// few != 0: that many partial sums stand in for the norm, and every workgroup adds them up as norm_finish_kernel does; the first leaves
-// the norm in *norm.
-__global__ __launch_bounds__(kThreads) void clip_kernel(const ClipTable b, const double* __restrict__ partials, const uint32_t few, double* __restrict__ norm,
+// FEW: `few` partial sums stand in for the norm, and every workgroup adds them up as norm_finish_kernel does; the first leaves the norm
+// in *norm.  Otherwise a norm that clips nothing ends the work in place before a value is read.
+template <bool FEW, class Table>
+__global__ __launch_bounds__(kThreads) void clip_kernel(const Table b, const double* __restrict__ partials, const uint32_t few, double* __restrict__ norm,
                                                         const double max_norm) {
-    double n;
-    if (few != 0u) {
-        n = norm_of_partials(partials, few);
-        if (blockIdx.x == 0u && threadIdx.x == 0u) *norm = n;
-    } else {
-        n = *norm;
-    }
-    const float c = clip_factor(n, max_norm);
+    float c = FEW ? 0.0f : clip_factor(*norm, max_norm);
+    bool have = !FEW;
+    const auto factor = [&] {
+        if (FEW && !have) {
+            const double n = norm_of_partials(partials, few);
+            if (blockIdx.x == 0u && threadIdx.x == 0u) *norm = n;
+            c = clip_factor(n, max_norm);
+            have = true;
+        }
+        return c;
+    };
     for (uint32_t piece = blockIdx.x; piece < b.pieces; piece += gridDim.x) {
         const uint32_t k = tensor_of_piece(b.start, b.count, piece);
         const uint64_t base = (uint64_t)(piece - b.start[k]) * kPiece;
@@ -160,9 +167,9 @@ __global__ __launch_bounds__(kThreads) void clip_kernel(const ClipTable b, const
         const uint32_t count = left < kPiece ? (uint32_t)left : kPiece;
         const void* x = b.data[k];
         void* y = b.out[k];
-        if (c == 1.0f && x == y) continue;   // in place and below the norm: every value is its own
+        if (!FEW && c == 1.0f && x == y) continue;   // every value is its own
         with_dtype(b.dtype[k], [&](auto in) {
-            with_dtype(b.out_dtype[k], [&](auto out) { clip_piece<in, out>(at<in>(x, base), at<out>(y, base), count, c); });
+            with_dtype(b.out_dtype[k], [&](auto out) { clip_piece<in, out>(at<in>(x, base), at<out>(y, base), count, factor); });
         });
     }
 }
@@ -197,19 +204,24 @@ uint32_t fill_table(Table& b, const mqg_clip_item* items, uint32_t first, uint32
 uint64_t norm_max_values() { return ((uint64_t)0x7FFFFFFF - MQG_MAX_NORM_TENSORS) * kPiece; }   // pieces of a launch fit 31 bits
 
 // the partial sums of all tensors; *stored: how many
+template <class Table>
 static hipError_t launch_partials(const mqg_clip_item* items, uint32_t count, bool once, double* partials, uint32_t* stored, hipStream_t stream) {
-    NormTable b;
+    Table b;
     *stored = 0;
     for (uint32_t i = 0; i < count;) {
         i = fill_table(b, items, i, count, [](uint32_t, const mqg_clip_item&) {});
         if (b.pieces == 0) continue;
         const uint32_t blocks = std::min(b.pieces, kNormBlocks);
-        hipLaunchKernelGGL((once ? norm_partial_kernel<true> : norm_partial_kernel<false>), dim3(blocks), dim3(kThreads), 0, stream, b, partials + *stored);
+        hipLaunchKernelGGL((once ? norm_partial_kernel<true, Table> : norm_partial_kernel<false, Table>), dim3(blocks), dim3(kThreads), 0, stream, b, partials + *stored);
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
         *stored += blocks;
     }
     return hipSuccess;
+}
+static hipError_t launch_partials(const mqg_clip_item* items, uint32_t count, bool once, double* partials, uint32_t* stored, hipStream_t stream) {
+    return count <= NormTableFew::kTensors ? launch_partials<NormTableFew>(items, count, once, partials, stored, stream)
+                                           : launch_partials<NormTable>(items, count, once, partials, stored, stream);
 }
 static hipError_t launch_finish(const double* partials, uint32_t stored, double* norm, hipStream_t stream) {
     hipLaunchKernelGGL(norm_finish_kernel, dim3(1), dim3(kThreads), 0, stream, partials, stored, norm);
@@ -222,21 +234,28 @@ hipError_t launch_global_norm(const mqg_clip_item* items, uint32_t count, double
     return e == hipSuccess ? launch_finish(partials, stored, norm, stream) : e;
 }
 
+template <class Table>
 static hipError_t launch_clip_pieces(const mqg_clip_item* items, uint32_t count, const double* partials, uint32_t few, double* norm, double max_norm,
                                      hipStream_t stream) {
-    ClipTable b;
+    Table b;
     for (uint32_t i = 0; i < count;) {
         i = fill_table(b, items, i, count, [&](uint32_t k, const mqg_clip_item& it) {
             b.out[k] = it.out;
             b.out_dtype[k] = (uint8_t)it.out_dtype;
         });
         if (b.pieces == 0) continue;
-        hipLaunchKernelGGL(clip_kernel, dim3(std::min(b.pieces, kMaxBlocks)), dim3(kThreads), 0, stream, b, partials, few, norm, max_norm);
+        hipLaunchKernelGGL((few != 0u ? clip_kernel<true, Table> : clip_kernel<false, Table>), dim3(std::min(b.pieces, kMaxBlocks)), dim3(kThreads), 0, stream, b, partials, few, norm, max_norm);
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
         few = 0;   // the first launch has left the norm
     }
     return hipSuccess;
+}
+
+static hipError_t launch_clip_pieces(const mqg_clip_item* items, uint32_t count, const double* partials, uint32_t few, double* norm, double max_norm,
+                                     hipStream_t stream) {
+    return count <= ClipTableFew::kTensors ? launch_clip_pieces<ClipTableFew>(items, count, partials, few, norm, max_norm, stream)
+                                           : launch_clip_pieces<ClipTable>(items, count, partials, few, norm, max_norm, stream);
 }
 
 hipError_t launch_clip(const mqg_clip_item* items, uint32_t count, const double* norm, double max_norm, hipStream_t stream) {

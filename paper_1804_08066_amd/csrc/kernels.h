@@ -232,7 +232,8 @@ hipError_t launch_sum_squares_batch(const SumSquaresBatch& b, uint32_t count, do
 // the same with the partial sums in a device array the library holds (no allocation, no workspace argument)
 hipError_t launch_sum_squares_batch_static(const SumSquaresBatch& b, uint32_t count, double* out, hipStream_t stream);
 
-// grad_norm.hip: tensors of one launch, of any of the three types.  A list longer than a table takes several launches.
+// grad_norm.hip: tensors of one launch, of any of the three types.  A list longer than a table takes several launches, and one that the
+// small table holds takes that (a launch's arguments are copied for every launch).
 template <uint32_t TENSORS>
 struct TensorTable {
     static constexpr uint32_t kTensors = TENSORS;
@@ -242,11 +243,15 @@ struct TensorTable {
     uint64_t n[TENSORS];
     uint8_t dtype[TENSORS];
 };
-using NormTable = TensorTable<192>;
-struct ClipTable : TensorTable<128> {
-    void* out[128];
-    uint8_t out_dtype[128];
+template <uint32_t TENSORS>
+struct OutTable : TensorTable<TENSORS> {
+    void* out[TENSORS];
+    uint8_t out_dtype[TENSORS];
 };
+using NormTable = TensorTable<192>;
+using NormTableFew = TensorTable<16>;
+using ClipTable = OutTable<128>;
+using ClipTableFew = OutTable<16>;
 constexpr uint32_t kNormBlocks = 2048;   // workgroups of a launch, and partial sums that it stores
 inline uint32_t norm_partials(uint32_t count) { return (count + NormTable::kTensors - 1u) / NormTable::kTensors * kNormBlocks; }
 uint64_t norm_max_values();              // of all tensors together
