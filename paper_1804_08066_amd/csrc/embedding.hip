@@ -79,10 +79,10 @@ struct Window {
 };
 
 // ---- lookup ------------------------------------------------------------------------------------------
-// `1 << shift` lanes hold a row's (or a slice of a row's) values, V each, of kLookups rows at a time; the slices of a row
-// are neighbouring workgroups, so that rows are read and written as a whole (all first slices first: half the memory channels
-// of rows of 8 KB).  Bound by the fabric between the caches and memory.  The rows are written with streaming stores: they are read next by another kernel,
-// mostly from memory, and stores that stay in the caches push the table out of them.
+// `1 << shift` lanes hold a row's (or a slice of a row's) values, V each, of kLookups rows at a time; the slices of a row are
+// neighbouring workgroups.  Bound by the fabric between the caches and memory: 131072 half-precision rows of 4096 values into fp32, 3.2 GB,
+// take 530 us.  The rows are written with streaming stores: stores that stay in the caches push the table out of them (40001 rows of 1531
+// values, most of them another shard's: 40 us with ordinary stores and a row at a time, 30.5 with streaming ones, 27.7 with two rows).
 constexpr uint32_t kLookups = 2;
 template <int IN, int OUT, bool WIDE>
 __global__ __launch_bounds__(kThreads) void embedding_kernel(const RowMatrix table, const TokenIds ids, const uint32_t dim, const uint32_t shift,
@@ -442,10 +442,14 @@ __global__ __launch_bounds__(kOneThreads) void sort_one_kernel(const SortArgs a,
 }
 
 // ---- a few positions ------------------------------------------------------------------------------------
-// Without a sort: every workgroup finds the positions of its position's row among all of them, and adds up their slice of
-// grad_out where its own is the first.  One launch of 5 us for 500 positions of 512 values, where sort, sums and joins take 16; 512
-// positions of 4096 values take 16.3 and 17.6, 1000 take 41 and 20.
-constexpr uint32_t kFewTokens = 512, kFewSum = 8, kFewRows = 1024;
+// Without a sort: every workgroup finds the positions of its position's row among all of them, a quarter a wave, and adds up their
+// slice of grad_out where its own is the first.  One launch, whose work is the square of the positions for every slice of 256 values.
+// kFewWork: below it this is faster than sort, sums and joins (half-precision rows into fp32, positions x values, this and those:
+// 500 x 512 4.9 and 16 us; 1000 x 1000 10.5 and 18.5; 2000 x 250 8.6 and 20; 4000 x 250 19 and 24; 2000 x 1000 20.5 and 20.5;
+// 4000 x 500 35 and 24).
+constexpr uint32_t kFewTokens = 4096, kFewSum = 8, kFewRows = 1024;
+constexpr uint64_t kFewWork = 16000000;
+bool few_positions(uint64_t tokens, uint32_t dim) { return tokens <= kFewTokens && tokens * tokens * ((dim + 255u) / 256u) <= kFewWork; }
 struct FewArgs {
     TokenIds ids;
     RowMatrix grad, out;
@@ -455,28 +459,40 @@ struct FewArgs {
     float scale;
     bool accumulate;
 };
-template <int IN, int OUT, bool WIDE>
+__device__ __forceinline__ uint32_t few_row(const TokenIds& t, uint32_t i, uint32_t rows) {
+    return t.wide ? row_of<true>(t, i, rows, true) : row_of<false>(t, i, rows, true);
+}
+// ITEMS: positions that a lane searches
+template <int IN, int OUT, uint32_t ITEMS>
 __global__ __launch_bounds__(kThreads) void sum_few_kernel(const FewArgs a) {
     constexpr int V = values_of(IN, OUT);
     constexpr uint32_t kWaves = kThreads / 64u;
-    __shared__ uint32_t s_key[kFewTokens], s_list[kFewTokens];
+    __shared__ uint16_t s_list[ITEMS * kThreads];
+    __shared__ uint32_t s_found[kWaves];
     __shared__ float s_sum[kWaves - 1u][64][V];
     __shared__ uint8_t s_named[kFewRows];
     const uint32_t count = (uint32_t)a.ids.count, rows = (uint32_t)a.out.rows, tid = threadIdx.x, lane = tid & 63u;
     const uint32_t wave = (uint32_t)__builtin_amdgcn_readfirstlane((int)(tid >> 6));
-    for (uint32_t i = tid; i < count; i += kThreads) s_key[i] = row_of<WIDE>(a.ids, i, rows, true);
+    const uint32_t items = (count + kThreads - 1u) / kThreads, first = wave * 64u * items;   // a wave's positions are consecutive
+    uint32_t key[ITEMS];
+#pragma unroll
+    for (uint32_t j = 0; j < ITEMS; ++j) {
+        const uint32_t at = first + j * 64u + lane;
+        key[j] = j < items && at < count ? few_row(a.ids, at, rows) : ~0u;
+    }
     if (blockIdx.x >= a.sums) {
         constexpr int VC = OUT == kF32 ? 4 : 8;
-        const uint64_t first = (uint64_t)(blockIdx.x - a.sums) * a.clear_rows, end = min(first + a.clear_rows, a.out.rows);
+        const uint64_t from = (uint64_t)(blockIdx.x - a.sums) * a.clear_rows, end = min(from + a.clear_rows, a.out.rows);
         for (uint32_t i = tid; i < a.clear_rows; i += kThreads) s_named[i] = 0u;
         __syncthreads();
-        for (uint32_t i = tid; i < count; i += kThreads) {
-            if (s_key[i] >= first && s_key[i] < end) s_named[s_key[i] - first] = 1u;
+#pragma unroll
+        for (uint32_t j = 0; j < ITEMS; ++j) {
+            if (key[j] >= from && key[j] < end) s_named[key[j] - from] = 1u;
         }
         __syncthreads();
         const float zero[VC] = {};
-        for (uint64_t row = first + (tid >> a.clear_shift); row < end; row += kThreads >> a.clear_shift) {
-            if (s_named[row - first] != 0u) continue;
+        for (uint64_t row = from + (tid >> a.clear_shift); row < end; row += kThreads >> a.clear_shift) {
+            if (s_named[row - from] != 0u) continue;
             for (uint32_t s = 0; s < a.clear_slices; ++s) {
                 const uint32_t col = ((s << a.clear_shift) + (tid & ((1u << a.clear_shift) - 1u))) * VC;
                 if (col < a.dim) Window<VC>(col, a.dim).template store_once<OUT>(at<OUT>(a.out.data, row * a.out.stride), zero, a.dim);
@@ -484,24 +500,38 @@ __global__ __launch_bounds__(kThreads) void sum_few_kernel(const FewArgs a) {
         }
         return;
     }
-    __syncthreads();
     const uint32_t p = blockIdx.x / a.slices, col = ((blockIdx.x - p * a.slices) * 64u + lane) * V;
-    const uint32_t k = s_key[p];
+    const uint32_t k = (uint32_t)__builtin_amdgcn_readfirstlane((int)few_row(a.ids, p, rows));
     if (k >= rows) return;
     const bool in = col < a.dim;
     const Window<V> w(in ? col : 0u, a.dim);
     Pack<OUT, V> old;
     void* y = at<OUT>(a.out.data, (uint64_t)k * a.out.stride);
-    uint32_t found = 0;
-    for (uint32_t i = 0; i < count; i += 64u) {
-        const bool mine = i + lane < count && s_key[i + lane] == k;
-        const uint64_t all = __builtin_amdgcn_ballot_w64(mine);
-        if (found == 0u && all != 0u && i + (uint32_t)__builtin_ctzll(all) < p) return;   // an earlier position's workgroup adds the row up
-        const uint32_t below = __builtin_amdgcn_mbcnt_hi((uint32_t)(all >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)all, 0u));
-        if (mine && wave == 0u) s_list[found + below] = i + lane;
-        found += (uint32_t)__builtin_popcountll(all);
-    }
     if (a.accumulate && wave == 0u && in) w.load(old, y, a.dim);
+    uint64_t match[ITEMS];
+    uint32_t found = 0;
+#pragma unroll
+    for (uint32_t j = 0; j < ITEMS; ++j) {
+        match[j] = __builtin_amdgcn_ballot_w64(key[j] == k);
+        if (match[j] != 0u && first + j * 64u + (uint32_t)__builtin_ctzll(match[j]) < p) found |= 1u << 31;   // not the first position of its row
+        found += (uint32_t)__builtin_popcountll(match[j]);
+    }
+    if (lane == 0u) s_found[wave] = found;
+    __syncthreads();
+    uint32_t before = 0;
+    found = 0;
+#pragma unroll
+    for (uint32_t n = 0; n < kWaves; ++n) {
+        if (n == wave) before = found;
+        found += s_found[n] & ~(1u << 31);
+        if (s_found[n] >> 31) return;
+    }
+#pragma unroll
+    for (uint32_t j = 0; j < ITEMS; ++j) {
+        const uint32_t below = __builtin_amdgcn_mbcnt_hi((uint32_t)(match[j] >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)match[j], 0u));
+        if (key[j] == k) s_list[before + below] = (uint16_t)(first + j * 64u + lane);
+        before += (uint32_t)__builtin_popcountll(match[j]);
+    }
     __syncthreads();
     float sum[V] = {};
     for (uint32_t n = wave; n < found; n += kWaves * kFewSum) {   // the waves take the positions in turn
@@ -796,7 +826,7 @@ struct GradWorkspace {
 };
 GradWorkspace grad_workspace(void* base, uint64_t tokens, uint32_t dim, uint64_t rows) {
     GradWorkspace w = {};
-    if (tokens <= kFewTokens) return w;
+    if (few_positions(tokens, dim)) return w;
     w.named = static_cast<uint32_t*>(base);
     if (tokens > kOneTokens) w.bytes = (rows + 15u) & ~(uint64_t)15u;
     const SortShape s = sort_shape(tokens, rows);
@@ -849,7 +879,7 @@ hipError_t launch_embedding_grad(const RowMatrix& grad_out, const TokenIds& ids,
         hipLaunchKernelGGL(clear_rows_kernel, dim3(clear_shape(clear.end).blocks / clear.slices), dim3(kThreads), 0, stream, clear);
         return hipGetLastError();
     }
-    if (ids.count <= kFewTokens) {
+    if (few_positions(ids.count, dim)) {
         FewArgs f = {};
         f.ids = ids;
         f.grad = grad_out;
@@ -868,7 +898,8 @@ hipError_t launch_embedding_grad(const RowMatrix& grad_out, const TokenIds& ids,
                 constexpr uint32_t width = 64u * values_of(in, o);
                 f.slices = (dim + width - 1u) / width;
                 f.sums = (uint32_t)ids.count * f.slices;
-                hipLaunchKernelGGL((ids.wide ? sum_few_kernel<in, o, true> : sum_few_kernel<in, o, false>), dim3(f.sums + clears), dim3(kThreads), 0, stream, f);
+                const auto kernel = ids.count <= 2u * kThreads ? sum_few_kernel<in, o, 2u> : (ids.count <= 8u * kThreads ? sum_few_kernel<in, o, 8u> : sum_few_kernel<in, o, 16u>);
+                hipLaunchKernelGGL(kernel, dim3(f.sums + clears), dim3(kThreads), 0, stream, f);
             });
         });
         return hipGetLastError();

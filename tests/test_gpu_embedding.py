@@ -160,7 +160,8 @@ def test_lookup_keeps_special_values():
 @pytest.mark.parametrize("out", TYPES, ids=str)
 @pytest.mark.parametrize("dtype", TYPES, ids=str)
 def test_gradient_types(dtype, out, accumulate):
-    for dim, rows, count, index in ((64, 50, 700, torch.int32), (37, 90, 3000, torch.int64), (520, 20, 90, torch.int64)):
+    for dim, rows, count, index in ((64, 50, 700, torch.int32), (37, 90, 3000, torch.int64), (520, 20, 90, torch.int64), (300, 60, 5000, torch.int32),
+                                    (36, 70, 9000, torch.int64)):
         g = matrix(count, dim, 11, dtype)
         ids = some_tokens("shards", count, rows).to(DEV, index)
         old = matrix(rows, dim, 12, out)
@@ -171,7 +172,7 @@ def test_gradient_types(dtype, out, accumulate):
 
 
 @pytest.mark.parametrize("kind", KINDS)
-@pytest.mark.parametrize("count", [1, 2, 63, 64, 65, 200, 511, 513, 1025, 2047, 2049, 5000, 20_000])
+@pytest.mark.parametrize("count", [1, 2, 63, 64, 65, 200, 511, 513, 1025, 2047, 2049, 4096, 4097, 8192, 8193, 20_000])
 def test_gradient_lengths(count, kind):
     for dim, rows in ((5, 300), (24, 7), (130, 1000)):
         g = matrix(count, dim, count, BF16)
@@ -182,7 +183,7 @@ def test_gradient_lengths(count, kind):
 @pytest.mark.parametrize("dim", [1, 2, 3, 7, 8, 9, 31, 64, 255, 256, 257, 1023, 1025, 2048, 2049, 5000])
 @pytest.mark.parametrize("dtype", [F32, F16], ids=str)
 def test_gradient_widths(dtype, dim):
-    for count, rows in ((50, 20), (3000, 40)):
+    for count, rows in ((50, 20), (700, 30), (3000, 40), (9000, 50)):
         g = matrix(count, dim, dim, dtype)
         ids = some_tokens("text", count, rows).to(DEV)
         check_grad(g, ids, mq.mqg_embedding_grad(g, ids, rows, scale=2.0, out=torch.full((rows, dim), 9.0, device=DEV)), rows, 2.0)
@@ -219,7 +220,7 @@ def test_gradient_equal_inputs_equal_bits(tokens):
         assert torch.equal(mq.mqg_embedding_grad(g, ids.to(index), 500, workspace=workspace), first)
 
 
-@pytest.mark.parametrize("tokens", [40, 700, 9000])
+@pytest.mark.parametrize("tokens", [40, 700, 5000, 9000])
 def test_positions_that_add_to_no_row_are_not_read_into_any(tokens):
     """Infinite and missing values at padded and foreign positions stay out of every row."""
     ids = some_tokens("shards", tokens, 60).to(DEV)
@@ -237,7 +238,7 @@ def test_positions_that_add_to_no_row_are_not_read_into_any(tokens):
     assert torch.isnan(got).sum() == 1 and torch.isnan(got[ids[at], 7])
 
 
-@pytest.mark.parametrize("tokens", [20, 600, 4000])
+@pytest.mark.parametrize("tokens", [20, 600, 5000, 12_000])
 def test_gradient_strides_alignment_and_leading_dimensions(tokens):
     wide = matrix(tokens, 100, 17, BF16)
     g = wide[:, 5:66]
@@ -297,7 +298,7 @@ def test_gradient_against_differences():
         assert abs((loss[0] - loss[1]) / step - grad[r, c].double()) <= 2 * 40 * 8 * 2.0 ** -24 * 3
 
 
-@pytest.mark.parametrize("tokens", [7, 800])
+@pytest.mark.parametrize("tokens", [7, 3000])
 def test_memory_past_four_gigavalues(tokens):
     """Offsets of a table of 4.5 * 10^9 values: rows at its end are looked up, and added to, where they are."""
     rows, dim = 1_100_000, 4096
@@ -313,7 +314,7 @@ def test_memory_past_four_gigavalues(tokens):
     check_grad(g, near, end, 1000, -0.1, old=old)
 
 
-@pytest.mark.parametrize("tokens", [50, 1500, 9000])
+@pytest.mark.parametrize("tokens", [50, 1500, 5000, 9000])
 def test_other_stream_and_replayed_graph(tokens):
     rows, dim = 700, 40
     g = matrix(tokens, dim, 24, BF16)

@@ -186,11 +186,11 @@ def test_embedding_arguments_are_checked():
     assert grad(out=rows(B, 0)) == mq.MQG_EINVAL
     assert grad(out=rows(B, 8, 15)) == mq.MQG_EINVAL
     assert grad(out=rows(A + 64)) == mq.MQG_EINVAL                       # over grad_out
-    many = dict(g=rows(A, 1000), ids=tokens(count=1000))                 # a few positions need no workspace
-    assert mq.mqg_embedding_grad_workspace_bytes(1000, 16, 8) > 0
+    many = dict(g=rows(A, 5000), ids=tokens(count=5000), out=rows(0x200000))   # a few positions need no workspace
+    assert mq.mqg_embedding_grad_workspace_bytes(5000, 16, 8) > 0
     assert grad(workspace=None, **many) == mq.MQG_EINVAL
-    assert grad(workspace=0x100008, **many) == mq.MQG_EALIGN
-    for over in (A, 0x1000, B):
+    assert grad(workspace=0x300008, **many) == mq.MQG_EALIGN
+    for over in (A, 0x1000, 0x200000):
         assert grad(workspace=over, **many) == mq.MQG_EINVAL
     assert lookup(ids=tokens(None, 0), out=rows(None, 0)) == mq.MQG_OK    # no tokens: nothing to do
     assert grad(g=rows(None, 0), ids=tokens(None, 0), accumulate=1, workspace=None) == mq.MQG_OK
