@@ -13,7 +13,9 @@
  *   mqg_mdp_*             the host-side agent that picks K  (the paper's MQGrad-SARSA)
  * and, further down: the server's re-quantizing step of the printed Algorithm 1 with the worker's
  * de-quantizing update, several layer tensors per launch, the footnote's deterministic [min, max]
- * encoder (per bucket or per tensor), and the Adaptive baseline's bit rule.
+ * encoder (per bucket or per tensor), and the Adaptive baseline's bit rule; and what a large model's
+ * gradients go through before the exchange: the norm of all tensors together, clipping, and the rows of
+ * an embedding table by token with their gradient.
  *
  * Conventions
  *   - Plain C ABI.  No function throws, aborts or allocates device memory.

@@ -120,6 +120,17 @@ def test_mixed_types_and_many_tensors():
     assert all(torch.equal(a, b) for a, b in zip(outputs, other))
 
 
+@pytest.mark.parametrize("count", [2, 16, 17, 40, 128, 129])
+def test_lists_around_a_launchs_tables(count):
+    tensors = [values(100 + 37 * k, k, TYPES[k % 3]) for k in range(count)]
+    outputs = [torch.zeros(t.numel(), device=DEV) for t in tensors]
+    _, norm = mq.mqg_clip_global_norm(tensors, 0.1, outputs=outputs)
+    assert_norm(norm, tensors)
+    assert mq.mqg_global_norm(tensors).item() == norm.item()
+    for t, o in zip(tensors, outputs):
+        assert_clipped(o, t, norm.item(), 0.1)
+
+
 def test_one_tensor_several_times_counts_several_times():
     t = values(5000, 4)
     assert_norm(mq.mqg_global_norm([t, t, t]), [t, t, t])
