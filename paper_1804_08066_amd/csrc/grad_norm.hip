@@ -175,9 +175,10 @@ __global__ __launch_bounds__(kThreads) void clip_kernel(const Table b, const dou
 }
 
 constexpr uint32_t kMaxBlocks = 1u << 23;   // a launch holds less than 2^32 lanes
-// So few partial sums are added up by every workgroup of the clipping kernel, without a launch in between (1.07 M values in ten tensors:
-// a launch of 4 us less).
-constexpr uint32_t kFewPartials = 512;
+// So few partial sums are added up by every one of so few workgroups of the clipping kernel, without a launch in between (half-precision
+// values into fp32: 3 M in ten tensors 13.2 -> 8.9 us, 8 M in sixty 20.9 -> 16.6, 40 M 56 -> 51; into half precision 13.7 -> 8.3, 18.1 -> 15.5,
+// 41.5 -> 42.3; 234 M into fp32 286 -> 299).
+constexpr uint32_t kFewPartials = kNormBlocks, kFewPieces = 16384;
 
 // fills `b` with the tensors from items[first] on, as many as fit; returns the next one
 template <class Table, class F>
@@ -263,14 +264,17 @@ hipError_t launch_clip(const mqg_clip_item* items, uint32_t count, const double*
 }
 
 hipError_t launch_clip_global_norm(const mqg_clip_item* items, uint32_t count, double max_norm, double* partials, double* norm, hipStream_t stream) {
-    uint64_t bytes = 0;
-    for (uint32_t i = 0; i < count; ++i) bytes += items[i].n * bytes_of(items[i].dtype);
+    uint64_t bytes = 0, pieces = 0;
+    for (uint32_t i = 0; i < count; ++i) {
+        bytes += items[i].n * bytes_of(items[i].dtype);
+        pieces += (items[i].n + kPiece - 1u) / kPiece;
+    }
     // Values that clipping may find in the last-level cache are read with ordinary loads: 0.2, 0.5 and 0.8 GB of half-precision values into
     // fp32 took 182, 308 and 686 us with streaming loads and take 170, 291 and 676; 2.4 GB 1567 and 1580.
     uint32_t stored;
     hipError_t e = launch_partials(items, count, bytes > (1ull << 30), partials, &stored, stream);
     if (e != hipSuccess) return e;
-    const bool few = stored > 0 && stored <= kFewPartials;
+    const bool few = stored > 0 && stored <= kFewPartials && pieces <= kFewPieces;
     if (!few) e = launch_finish(partials, stored, norm, stream);
     return e == hipSuccess ? launch_clip_pieces(items, count, partials, few ? stored : 0u, norm, max_norm, stream) : e;
 }
