@@ -445,7 +445,7 @@ __global__ __launch_bounds__(kOneThreads) void sort_one_kernel(const SortArgs a,
 // Without a sort: every workgroup finds the positions of its position's row among all of them, a quarter a wave, and adds up their
 // slice of grad_out where its own is the first.  One launch, whose work is the square of the positions for every slice of 256 values.
 // kFewWork: below it this is faster than sort, sums and joins (half-precision rows into fp32, positions x values, this and those:
-// 500 x 512 4.9 and 16 us; 1000 x 1000 10.5 and 18.5; 2000 x 250 8.6 and 20; 4000 x 250 19 and 24; 2000 x 1000 20.5 and 20.5;
+// 500 x 512 4.9 and 16 us; 1000 x 1000 8.9 and 18.5; 2000 x 250 8.6 and 20; 4000 x 250 19 and 24; 2000 x 1000 20.5 and 20.5;
 // 4000 x 500 35 and 24).
 constexpr uint32_t kFewTokens = 4096, kFewSum = 8, kFewRows = 1024;
 constexpr uint64_t kFewWork = 16000000;
@@ -465,7 +465,7 @@ struct FewArgs {
 __device__ __forceinline__ uint32_t few_row(const TokenIds& t, uint32_t i, uint32_t rows) {
     return t.wide ? row_of<true>(t, i, rows, true) : row_of<false>(t, i, rows, true);
 }
-// ITEMS: positions that a lane searches
+// ITEMS: positions that a lane searches at most (1000 positions of 1000 values, 8 and 4: 10.7 and 8.9 us)
 template <int IN, int OUT, uint32_t ITEMS>
 __global__ __launch_bounds__(kThreads) void sum_few_kernel(const FewArgs a) {
     constexpr int V = values_of(IN, OUT);
@@ -922,7 +922,8 @@ hipError_t launch_embedding_grad(const RowMatrix& grad_out, const TokenIds& ids,
                 constexpr uint32_t width = 64u * values_of(in, o);
                 f.slices = (dim + width - 1u) / width;
                 f.sums = (uint32_t)ids.count * f.slices;
-                const auto kernel = ids.count <= 2u * kThreads ? sum_few_kernel<in, o, 2u> : (ids.count <= 8u * kThreads ? sum_few_kernel<in, o, 8u> : sum_few_kernel<in, o, 16u>);
+                const auto kernel = ids.count <= 4u * kThreads ? (ids.count <= 2u * kThreads ? sum_few_kernel<in, o, 2u> : sum_few_kernel<in, o, 4u>)
+                                                               : (ids.count <= 8u * kThreads ? sum_few_kernel<in, o, 8u> : sum_few_kernel<in, o, 16u>);
                 hipLaunchKernelGGL(kernel, dim3(f.sums + clears), dim3(kThreads), 0, stream, f);
             });
         });
