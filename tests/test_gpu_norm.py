@@ -100,6 +100,18 @@ def test_clip_in_place(dtype, ratio):
             assert torch.equal(t, b)
 
 
+@pytest.mark.parametrize("ratio", [0.5, 1.5])
+@pytest.mark.parametrize("n", [1 << 24, (1 << 24) + 1])
+def test_clip_in_place_around_the_length_where_the_norm_is_finished_first(n, ratio):
+    tensors = [values(n - 8192, 31, BF16), values(8192, 32, BF16)]
+    before = [t.clone() for t in tensors]
+    max_norm = ratio * exact_norm(tensors)
+    _, norm = mq.mqg_clip_global_norm(tensors, max_norm)
+    assert_norm(norm, before)
+    for t, b in zip(tensors, before):
+        assert_clipped(t, b, norm.item(), max_norm)
+
+
 def test_mixed_types_and_many_tensors():
     """More tensors than one launch takes, of all types and odd sizes, slices that are aligned to one value only."""
     rng = np.random.default_rng(3)
