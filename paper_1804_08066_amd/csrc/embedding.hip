@@ -358,59 +358,135 @@ __global__ __launch_bounds__(kSortThreads) void sort_scatter_kernel(const SortAr
     }
 }
 
-// The same in one workgroup, for batches that it holds: the digits' counts, the scatters and the keys between them stay in LDS.
-// A launch of the passes above mostly waits for memory and for the launch before it: the gradient of 4096 positions of 1024 values
-// took 37 us with them and takes 27, of which the sort 12; of 8192 positions 41 and 39; of 16384, in a workgroup that holds them, 66
-// instead of 51.
-constexpr uint32_t kOneThreads = 1024, kOneWaves = kOneThreads / 64u, kOneItems = 8, kOneTokens = kOneThreads * kOneItems;
-template <bool WIDE>
-__global__ __launch_bounds__(kOneThreads) void sort_one_kernel(const SortArgs a, const ClearRows c, const uint32_t passes) {
-    __shared__ uint32_t s_key[kOneTokens];
-    __shared__ uint16_t s_order[kOneTokens], s_wave[kOneWaves][kMaxDigits];
-    __shared__ uint32_t s_total[kOneWaves];
-    if (blockIdx.x > 0u) {
-        clear_rows(c, blockIdx.x - 1u, gridDim.x - 1u);
+// Batches that a workgroup holds are sorted by one launch: kBuckets workgroups read all positions, and each keeps those of its bucket, a
+// row's remainder, and sorts them by the quotient in LDS.  Where its bucket begins is the number of positions of the buckets before, which
+// it sees on the way.  So no workgroup waits for another, and the chain of count and scatter launches, each of which mostly waits for
+// memory and for the one before it, is gone.  Rows come out grouped, not in order, and positions that add to none last, which is all that
+// the sums ask for.  (The gradient of 5000 positions of 64 values, those launches and this one: 26 and 20.5 us, of which this 7.2; 12000 33.5
+// and 23.8; 16384 of 1024 44 and 39; with 206 MB of rows cleared 54 and 51.5.)  Digits of 8 bits: the LDS of two workgroups fits a CU, so
+// that rows are cleared beside.
+constexpr uint32_t kOneThreads = 1024, kOneWaves = kOneThreads / 64u, kOneItems = 16, kOneTokens = kOneThreads * kOneItems;
+constexpr uint32_t kBuckets = 256, kOneBits = 8, kOneDigits = 1u << kOneBits, kOneNamed = 1024;   // kOneNamed: quotients that have a flag in LDS
+constexpr uint32_t kPositionBits = 14;   // of an entry, whose other bits are the quotient
+static_assert(kOneNamed == kOneThreads, "a lane writes a flag");
+static_assert(kOneTokens <= 1u << kPositionBits, "a position does not fit an entry");
+bool one_sort(uint64_t tokens, uint64_t rows) { return tokens <= kOneTokens && (rows + kBuckets - 1u) / kBuckets < 1u << (32u - kPositionBits); }
+
+// Buckets of up to so many positions are sorted by counting the smaller entries of each: 64 compared by one ballot.  (5000 positions of which
+// one row has 400: the sort takes 11 us where 512 are compared, 7.2 where 64, 128 or 192 are, 8.7 with digits alone.)
+constexpr uint32_t kOneCompared = 128;
+
+// none: the quotient behind the rows', by which the last bucket sorts the positions that add to no row; bits, passes: of the quotients
+template <bool WIDE, uint32_t ITEMS>
+__global__ __launch_bounds__(kOneThreads) void sort_buckets_kernel(const SortArgs a, const ClearRows c, const uint32_t none, const uint32_t passes) {
+    __shared__ uint32_t s_entry[ITEMS * kOneThreads];
+    __shared__ uint16_t s_wave[kOneWaves][kOneDigits];
+    __shared__ uint32_t s_mine[kOneWaves], s_below[kOneWaves], s_total[kOneWaves];
+    __shared__ uint8_t s_named[kOneNamed];
+    if (blockIdx.x >= kBuckets) {
+        clear_rows(c, blockIdx.x - kBuckets, gridDim.x - kBuckets);
         return;
     }
-    const uint32_t digits = 1u << a.bits, tid = threadIdx.x, lane = tid & 63u, wave = tid >> 6, count = (uint32_t)a.ids.count;
-    const uint32_t items = (count + kOneThreads - 1u) / kOneThreads, first = wave * 64u * items + lane;   // a wave's keys are consecutive
-    if (tid < kJoinLists) a.join_counts[tid * kJoinLine] = 0u;
-    uint32_t key[kOneItems], from[kOneItems], rank[kOneItems];
+    const uint32_t tid = threadIdx.x, lane = tid & 63u, all = (uint32_t)a.ids.count, rows = (uint32_t)a.rows, bucket = blockIdx.x;
+    const uint32_t wave = (uint32_t)__builtin_amdgcn_readfirstlane((int)(tid >> 6));
+    const auto below_lane = [](uint64_t m) { return __builtin_amdgcn_mbcnt_hi((uint32_t)(m >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)m, 0u)); };
+    if (bucket == 0u && tid < kJoinLists) a.join_counts[tid * kJoinLine] = 0u;
+    s_named[tid] = 0u;
+    uint32_t count = 0, base = 0;
+    {
+        const uint32_t items = (all + kOneThreads - 1u) / kOneThreads, first = wave * 64u * items + lane;   // a wave's positions are consecutive
+        uint32_t key[ITEMS];
 #pragma unroll
-    for (uint32_t j = 0; j < kOneItems; ++j) {
-        from[j] = first + j * 64u;
-        key[j] = j < items && from[j] < count ? row_of<WIDE>(a.ids, from[j], a.rows, true) : 0u;
+        for (uint32_t j = 0; j < ITEMS; ++j) key[j] = row_of<WIDE>(a.ids, min(first + j * 64u, all - 1u), rows, true);
+        uint64_t own[ITEMS];
+        uint32_t mine = 0, below = 0;
+#pragma unroll
+        for (uint32_t j = 0; j < ITEMS; ++j) {
+            const bool valid = j < items && first + j * 64u < all;
+            const uint32_t of = key[j] < rows ? key[j] % kBuckets : kBuckets - 1u;
+            own[j] = __builtin_amdgcn_ballot_w64(valid && of == bucket);
+            mine += (uint32_t)__builtin_popcountll(own[j]);
+            below += (uint32_t)__builtin_popcountll(__builtin_amdgcn_ballot_w64(valid && of < bucket));
+        }
+        if (lane == 0u) {
+            s_mine[wave] = mine;
+            s_below[wave] = below;
+        }
+        __syncthreads();
+        uint32_t to = 0;
+#pragma unroll
+        for (uint32_t w = 0; w < kOneWaves; ++w) {
+            if (w == wave) to = count;
+            count += s_mine[w];
+            base += s_below[w];
+        }
+#pragma unroll
+        for (uint32_t j = 0; j < ITEMS; ++j) {
+            if ((own[j] >> lane) & 1u) {
+                const uint32_t quotient = key[j] < rows ? key[j] / kBuckets : none;
+                s_entry[to + below_lane(own[j])] = quotient << kPositionBits | (first + j * 64u);
+                if (quotient < kOneNamed) s_named[quotient] = 1u;
+            }
+            to += (uint32_t)__builtin_popcountll(own[j]);
+        }
+        __syncthreads();
     }
+    if (a.named != nullptr) {
+        const uint32_t row = tid * kBuckets + bucket;
+        if (tid < none && row < rows) reinterpret_cast<uint8_t*>(a.named)[row] = s_named[tid];
+    }
+    const auto put = [&](uint32_t to, uint32_t entry) {
+        const uint32_t quotient = entry >> kPositionBits;
+        a.keys_out[base + to] = quotient == none ? rows : quotient * kBuckets + bucket;
+        a.order_out[base + to] = entry & ((1u << kPositionBits) - 1u);
+    };
+    if (count <= kOneCompared) {
+        uint32_t other[kOneCompared / 64u];
+#pragma unroll
+        for (uint32_t j = 0; j < kOneCompared / 64u; ++j) other[j] = j * 64u + lane < count ? s_entry[j * 64u + lane] : ~0u;
+        for (uint32_t i = wave; i < count; i += kOneWaves) {
+            const uint32_t entry = (uint32_t)__builtin_amdgcn_readfirstlane((int)s_entry[i]);
+            uint32_t to = 0;
+#pragma unroll
+            for (uint32_t j = 0; j < kOneCompared / 64u; ++j) {
+                if (j * 64u < count) to += (uint32_t)__builtin_popcountll(__builtin_amdgcn_ballot_w64(other[j] < entry));
+            }
+            if (lane == 0u) put(to, entry);
+        }
+        return;
+    }
+    const uint32_t digits = 1u << a.bits, items = (count + kOneThreads - 1u) / kOneThreads, first = wave * 64u * items + lane;
+    uint32_t entry[ITEMS], rank[ITEMS];
     for (uint32_t pass = 0; pass < passes; ++pass) {
-        const uint32_t shift = pass * a.bits;
+        const uint32_t shift = kPositionBits + pass * a.bits;
         for (uint32_t d = lane; d < digits; d += 64u) s_wave[wave][d] = 0u;
         __builtin_amdgcn_wave_barrier();
 #pragma unroll
-        for (uint32_t j = 0; j < kOneItems; ++j) {
+        for (uint32_t j = 0; j < ITEMS; ++j) {
             if (j >= items) break;
-            const uint32_t d = (key[j] >> shift) & (digits - 1u);
-            const bool valid = first + j * 64u < count;
-            rank[j] = rank_in_wave(s_wave[wave], d, a.bits, valid);
+            const uint32_t i = first + j * 64u;
+            entry[j] = i < count ? s_entry[i] : 0u;
+            rank[j] = rank_in_wave(s_wave[wave], (entry[j] >> shift) & (digits - 1u), a.bits, i < count);
         }
         __syncthreads();
-        uint32_t all = 0;   // of digit tid
+        uint32_t total = 0;   // of digit tid
         if (tid < digits) {
 #pragma unroll
             for (uint32_t w = 0; w < kOneWaves; ++w) {
                 const uint32_t n = s_wave[w][tid];
-                s_wave[w][tid] = (uint16_t)all;
-                all += n;
+                s_wave[w][tid] = (uint16_t)total;
+                total += n;
             }
         }
-        uint32_t upto = all;
+        uint32_t upto = total;
 #pragma unroll
         for (uint32_t m = 1; m < 64u; m <<= 1) {
-            const uint32_t other = __shfl_up(upto, m, 64);
-            if (lane >= m) upto += other;
+            const uint32_t before = __shfl_up(upto, m, 64);
+            if (lane >= m) upto += before;
         }
         if (lane == 63u) s_total[wave] = upto;
         __syncthreads();
-        uint32_t before = upto - all;
+        uint32_t before = upto - total;
         for (uint32_t w = 0; w < wave; ++w) before += s_total[w];
         if (tid < digits) {
 #pragma unroll
@@ -418,26 +494,14 @@ __global__ __launch_bounds__(kOneThreads) void sort_one_kernel(const SortArgs a,
         }
         __syncthreads();
 #pragma unroll
-        for (uint32_t j = 0; j < kOneItems; ++j) {
+        for (uint32_t j = 0; j < ITEMS; ++j) {
             if (j >= items) break;
             if (first + j * 64u >= count) continue;
-            const uint32_t to = s_wave[wave][(key[j] >> shift) & (digits - 1u)] + rank[j];
-            s_key[to] = key[j];
-            s_order[to] = (uint16_t)from[j];
+            const uint32_t to = s_wave[wave][(entry[j] >> shift) & (digits - 1u)] + rank[j];
+            if (pass + 1u < passes) s_entry[to] = entry[j];
+            else put(to, entry[j]);
         }
         __syncthreads();
-#pragma unroll
-        for (uint32_t j = 0; j < kOneItems; ++j) {
-            const uint32_t i = first + j * 64u;
-            if (j >= items) break;
-            if (i >= count) continue;
-            key[j] = s_key[i];
-            from[j] = s_order[i];
-            if (pass + 1u == passes) {
-                a.keys_out[i] = key[j];
-                a.order_out[i] = from[j];
-            }
-        }
     }
 }
 
@@ -673,7 +737,7 @@ __device__ __forceinline__ void sum_chunks(const SumArgs& a, const uint64_t bloc
     const bool tail = last < rows && key(end) == last && is_long(end, last);
     const uint64_t chunk = block * per + team;
     list_runs(a, slice == 0u && lane == 0u && tail && !(continues && cur == last), (uint32_t)chunk, last);
-    if (cur >= rows || col >= a.dim) return;               // keys rise: no position from here on adds to a row
+    if (cur >= rows || col >= a.dim) return;               // such keys are the last: no position from here on adds to a row
     uint32_t i = start, stop = end;
     if (continues && !head) {                              // the chunk before this one adds it up
         while (i < end && key(i) == cur) ++i;
@@ -740,11 +804,15 @@ __device__ __forceinline__ void sum_chunks(const SumArgs& a, const uint64_t bloc
     finish();
 }
 template <int IN, int OUT, bool UNIFORM, bool ACCUMULATE>
-__global__ __launch_bounds__(kThreads) void sum_runs_kernel(const SumArgs a) {
+__global__ __launch_bounds__(kThreads) void sum_runs_kernel(const SumArgs a, const ClearRows c, const uint32_t sums) {
+    if (blockIdx.x >= sums) {
+        if constexpr (!ACCUMULATE) clear_rows<OUT>(c, blockIdx.x - sums, gridDim.x - sums);
+        return;
+    }
     __shared__ uint32_t s_key[kMostPositions + 2u * kMostChunk + 2u], s_order[kMostPositions + kMostChunk];
     const uint32_t first = blockIdx.x / a.slices, slice = blockIdx.x - first * a.slices;
     const uint64_t blocks = (a.count + (uint64_t)(kThreads >> a.shift) * a.chunk - 1u) / ((kThreads >> a.shift) * a.chunk);
-    for (uint64_t block = first; block < blocks; block += gridDim.x / a.slices) {
+    for (uint64_t block = first; block < blocks; block += sums / a.slices) {
         sum_chunks<IN, OUT, UNIFORM, ACCUMULATE>(a, block, slice, s_key, s_order);
         __syncthreads();
     }
@@ -852,7 +920,7 @@ GradWorkspace grad_workspace(void* base, uint64_t tokens, uint32_t dim, uint64_t
     GradWorkspace w = {};
     if (few_positions(tokens, dim, rows)) return w;
     w.named = static_cast<uint32_t*>(base);
-    if (tokens > kOneTokens) w.bytes = (rows + 15u) & ~(uint64_t)15u;
+    w.bytes = (rows + 15u) & ~(uint64_t)15u;
     const SortShape s = sort_shape(tokens, rows);
     char* p = static_cast<char*>(base);
     const auto take = [&](uint64_t words) {
@@ -952,18 +1020,29 @@ hipError_t launch_embedding_grad(const RowMatrix& grad_out, const TokenIds& ids,
         return (uint32_t)std::min<uint64_t>(kClearBlocks, clear.end - clear.first);
     };
     hipError_t e;
-    if (ids.count <= kOneTokens) {
+    const uint32_t none = (uint32_t)((table_grad.rows + kBuckets - 1u) / kBuckets);
+    uint32_t none_bits = 1;
+    while ((none >> none_bits) != 0u) ++none_bits;
+    // Where rows are cleared and a bucket's have flags, the sums' launch clears those that no position names; otherwise the launches below do.
+    const bool one = one_sort(ids.count, table_grad.rows) && (accumulate || none <= kOneNamed);
+    if (one) {
+        const uint32_t passes = (none_bits + kOneBits - 1u) / kOneBits;
+        a.bits = (none_bits + passes - 1u) / passes;
         a.keys_out = w.keys[0];
         a.order_out = w.order[0];
-        a.named = nullptr;
-        const uint32_t more = share(true);
-        hipLaunchKernelGGL((ids.wide ? sort_one_kernel<true> : sort_one_kernel<false>), dim3(1u + more), dim3(kOneThreads), 0, stream, a, clear, s.passes);
+        const bool small = ids.count <= kOneTokens / 2u;
+        const auto kernel = ids.wide ? (small ? sort_buckets_kernel<true, kOneItems / 2u> : sort_buckets_kernel<true, kOneItems>)
+                                     : (small ? sort_buckets_kernel<false, kOneItems / 2u> : sort_buckets_kernel<false, kOneItems>);
+        // (50257 rows of 64 values: 20.5 us without any beside, 21.7 with)
+        const uint32_t more = left > 2u * beside ? share(false) : 0u;
+        hipLaunchKernelGGL(kernel, dim3(kBuckets + more), dim3(kOneThreads), 0, stream, a, clear, none, passes);
         e = hipGetLastError();
         if (e != hipSuccess) return e;
         a.keys = a.keys_out;
         a.order = a.order_out;
+        clear.named = reinterpret_cast<const uint8_t*>(a.named);
     }
-    for (uint32_t pass = 0; ids.count > kOneTokens && pass < s.passes; ++pass) {
+    for (uint32_t pass = 0; !one && pass < s.passes; ++pass) {
         a.keys_out = w.keys[pass & 1u];
         a.order_out = w.order[pass & 1u];
         a.shift = pass * s.bits;
@@ -994,6 +1073,9 @@ hipError_t launch_embedding_grad(const RowMatrix& grad_out, const TokenIds& ids,
     b.scale = scale;
     b.accumulate = accumulate;
     const uint64_t chunks = (ids.count + b.chunk - 1u) / b.chunk;
+    clear.first = 0;
+    clear.end = left;
+    const uint32_t clears = left == 0u ? 0u : clear_shape(left).blocks / clear.slices;
     with_dtype(grad_out.dtype, [&](auto in) {
         with_dtype(table_grad.dtype, [&](auto o) {
             constexpr uint32_t v = values_of(in, o);
@@ -1002,7 +1084,7 @@ hipError_t launch_embedding_grad(const RowMatrix& grad_out, const TokenIds& ids,
             b.slices = g.slices;
             const auto kernel = accumulate ? (g.shift >= 6u ? sum_runs_kernel<in, o, true, true> : sum_runs_kernel<in, o, false, true>)
                                            : (g.shift >= 6u ? sum_runs_kernel<in, o, true, false> : sum_runs_kernel<in, o, false, false>);
-            hipLaunchKernelGGL(kernel, dim3(g.blocks), dim3(kThreads), 0, stream, b);
+            hipLaunchKernelGGL(kernel, dim3(g.blocks + clears), dim3(kThreads), 0, stream, b, clear, g.blocks);
         });
     });
     e = hipGetLastError();

@@ -31,7 +31,7 @@ KERNELS = ("requantize_tensor_cells_kernel", "sum_range_cells_kernel", "requanti
            "quantize_minmax_tensors_kernel", "quantize_minmax_wave_kernel", "quantize_minmax_kernel",
            "quantize_tensors_wave_kernel", "quantize_tensors_cells_kernel", "quantize_tensors_kernel", "quantize_wave_kernel",
            "quantize_cells_kernel", "quantize_pack_kernel", "norm_partial_kernel", "norm_finish_kernel", "clip_kernel", "embedding_kernel",
-           "sort_count_kernel", "sort_one_kernel", "sum_few_kernel", "sort_scatter_kernel", "clear_rows_kernel", "sum_runs_kernel", "join_runs_kernel", "stream_quantize_kernel", "stream_update_kernel", "range_",
+           "sort_count_kernel", "sort_buckets_kernel", "sum_few_kernel", "sort_scatter_kernel", "clear_rows_kernel", "sum_runs_kernel", "join_runs_kernel", "stream_quantize_kernel", "stream_update_kernel", "range_",
            "clear_", "finish_", "fold_")
 
 

@@ -172,7 +172,7 @@ def test_gradient_types(dtype, out, accumulate):
 
 
 @pytest.mark.parametrize("kind", KINDS)
-@pytest.mark.parametrize("count", [1, 2, 63, 64, 65, 200, 511, 513, 1024, 1025, 2047, 2049, 4096, 4097, 8192, 8193, 20_000])
+@pytest.mark.parametrize("count", [1, 2, 63, 64, 65, 200, 511, 513, 1024, 1025, 2047, 2049, 4096, 4097, 8192, 8193, 16_384, 16_385, 20_000])
 def test_gradient_lengths(count, kind):
     for dim, rows in ((5, 300), (24, 7), (130, 1000)):
         g = matrix(count, dim, count, BF16)
@@ -199,6 +199,22 @@ def test_gradient_tables(rows):
         ids = ids.to(DEV)
         g = matrix(count, 3, 13)
         check_grad(g, ids, mq.mqg_embedding_grad(g, ids, rows), rows, 1.0)
+
+
+@pytest.mark.parametrize("accumulate", [False, True])
+@pytest.mark.parametrize("rows", [511, 60_000, 65_281, 262_144, 262_145, 600_000])
+@pytest.mark.parametrize("count", [5000, 16_384])
+def test_gradient_where_the_remainders_by_256_are_few(count, rows, accumulate):
+    """Rows that lie a multiple of 256 apart come together in the sort: all of them, none, and more than it compares with each other."""
+    for used in ([7], [0, 255], [3, 4, 5, 200, 254]):
+        quotients = some_tokens("text", count, (rows + 255) // 256, seed=count)
+        ids = quotients * 256 + torch.tensor(used)[torch.arange(count) % len(used)]   # some behind the last row
+        ids[::11] = -5
+        ids = ids.to(DEV)
+        g, old = matrix(count, 4, 14), matrix(rows, 4, 15)
+        out = old.clone()
+        mq.mqg_embedding_grad(g, ids, rows, scale=-1.5, out=out, accumulate=accumulate)
+        check_grad(g, ids, out, rows, -1.5, old=old if accumulate else None)
 
 
 @pytest.mark.parametrize("kind", KINDS)
