@@ -509,8 +509,8 @@ __global__ __launch_bounds__(kOneThreads) void sort_buckets_kernel(const SortArg
 // Without a sort: every workgroup finds the positions of its position's row among all of them, a quarter a wave, and adds up their
 // slice of grad_out where its own is the first.  One launch, whose work is the square of the positions for every slice of 256 values.
 // kFewWork: below it this is faster than sort, sums and joins (half-precision rows into fp32, positions x values, this and those:
-// 500 x 512 4.9 and 16 us; 1000 x 1000 8.9 and 18.5; 2000 x 250 8.6 and 20; 4000 x 250 19 and 24; 2000 x 1000 20.5 and 20.5;
-// 4000 x 500 35 and 24).
+// 1000 x 1000 8.9 and 17.7 us; 2000 x 64 8.8 and 19.7; 2000 x 500 11.9 and 19; 3300 x 250 16.4 and 20.6; 4000 x 250 19 and 20.6;
+// 2000 x 1000 21 and 19.7; 2600 x 500 21 and 19.8).
 constexpr uint32_t kFewTokens = 4096, kFewSum = 8, kFewRows = 1024;
 constexpr uint64_t kFewWork = 16000000;
 // Few rows of the table have long runs, which one workgroup adds up (2000 positions of 64 values in 4 rows: 29 us against 16).
