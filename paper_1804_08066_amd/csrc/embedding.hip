@@ -1050,6 +1050,8 @@ hipError_t launch_embedding_grad(const RowMatrix& grad_out, const TokenIds& ids,
         uint32_t more = share(false);
         if (a.named != nullptr) more = std::max<uint32_t>(more, (uint32_t)std::min<uint64_t>(kClearBlocks, a.rows / (32u * kSortThreads)));
         hipLaunchKernelGGL((ids.wide ? sort_count_kernel<true> : sort_count_kernel<false>), dim3(s.ranges + more), dim3(kSortThreads), 0, stream, a, clear);
+        e = hipGetLastError();   // counts that nothing wrote would scatter anywhere
+        if (e != hipSuccess) return e;
         more = share(pass + 1u == s.passes);
         hipLaunchKernelGGL((ids.wide ? sort_scatter_kernel<true> : sort_scatter_kernel<false>), dim3(s.ranges + more), dim3(kSortThreads), 0, stream, a, clear);
         e = hipGetLastError();
