@@ -492,7 +492,8 @@ mqg_status mqg_embedding(const mqg_rows* table, const mqg_tokens* tokens, uint32
 /* grad_out: tokens->count rows, read; table_grad: `rows` rows, overwritten or added to.
  *   workspace   device, mqg_embedding_grad_workspace_bytes(tokens->count, dim, table_grad->rows) bytes of scratch memory, 16-byte
  *               aligned; contents on entry are of no interest, contents on return are unspecified.  Calls that share a
- *               workspace must not overlap.  May be NULL where that size is 0.
+ *               workspace must not overlap.  May be NULL where that size is 0.  The size for the largest of several batches
+ *               is enough for each: it does not fall as any of the three grows.
  * Errors as for mqg_embedding. */
 size_t mqg_embedding_grad_workspace_bytes(uint64_t tokens, uint32_t dim, uint64_t rows);
 mqg_status mqg_embedding_grad(const mqg_rows* grad_out, const mqg_tokens* tokens, uint32_t dim, float scale, const mqg_rows* table_grad,

@@ -809,7 +809,7 @@ mqg_status mqg_embedding_grad(const mqg_rows* grad_out, const mqg_tokens* tokens
     if (st == MQG_OK) st = rows_args(table_grad, MQG_MAX_TABLE_ROWS, dim, true, o);
     if (st != MQG_OK) return st;
     if (table_grad->rows == 0u || grad_out->rows != tokens->count) return MQG_EINVAL;
-    const size_t need = mqg::embedding_grad_workspace(ids.count, dim, o.rows);
+    const size_t need = mqg::embedding_grad_takes_workspace(ids.count, dim, o.rows) ? mqg::embedding_grad_workspace(ids.count, dim, o.rows) : 0;
     if (need != 0 && workspace == nullptr) return MQG_EINVAL;
     if (misaligned(workspace, 16u)) return MQG_EALIGN;
     const Span out = span_of(*table_grad, dim), in = span_of(*grad_out, dim), at = span_of(*tokens), scratch = span_of(workspace, need);

@@ -163,6 +163,7 @@ constexpr uint32_t kClearBlocks = 2048;          // what the GPU holds, twice ov
 struct SortShape {
     uint32_t passes, bits, ranges;
     uint64_t range;                       // positions of one, a multiple of kSortTile
+    uint64_t most_counts;                 // no fewer than ranges << bits, here and for fewer positions and rows
 };
 SortShape sort_shape(uint64_t tokens, uint64_t rows) {
     SortShape s;
@@ -174,6 +175,7 @@ SortShape sort_shape(uint64_t tokens, uint64_t rows) {
     const uint64_t most = std::min<uint64_t>(kMaxRanges, std::max<uint64_t>(kRanges, tiles / kRangeTiles)), each = (tiles + most - 1u) / most;
     s.range = each * kSortTile;
     s.ranges = (uint32_t)((tokens + s.range - 1u) / s.range);
+    s.most_counts = std::min(tiles, most) << std::min(all, kMaxDigitBits);
     return s;
 }
 
@@ -514,8 +516,9 @@ __global__ __launch_bounds__(kOneThreads) void sort_buckets_kernel(const SortArg
 constexpr uint32_t kFewTokens = 4096, kFewSum = 8, kFewRows = 1024;
 constexpr uint64_t kFewWork = 16000000;
 // Few rows of the table have long runs, which one workgroup adds up (2000 positions of 64 values in 4 rows: 29 us against 16).
+constexpr uint32_t kFewRun = 256;   // positions of a row, on average
 bool few_positions(uint64_t tokens, uint32_t dim, uint64_t rows) {
-    return tokens <= kFewTokens && tokens <= 256u * rows && tokens * tokens * ((dim + 255u) / 256u) <= kFewWork;
+    return tokens <= kFewTokens && tokens <= kFewRun * rows && tokens * tokens * ((dim + 255u) / 256u) <= kFewWork;
 }
 struct FewArgs {
     TokenIds ids;
@@ -653,6 +656,7 @@ __global__ __launch_bounds__(kThreads) void sum_few_kernel(const FewArgs a) {
 // the rows read and written).
 constexpr uint32_t kRows = 8;         // in flight
 constexpr uint32_t kMostChunk = 64, kMostPositions = 2048;   // of a chunk, and of a workgroup's chunks together
+constexpr uint32_t kShortestChunk = kMostPositions / kThreads;
 
 struct SumArgs {
     const uint32_t *keys, *order;
@@ -902,12 +906,21 @@ uint32_t chunk_of(uint64_t tokens, uint32_t dim) {
     const RowShape g = row_shape(1, dim, 8u);
     const uint32_t per = kThreads >> g.shift;                       // most chunks of a workgroup: 8 values a lane
     const uint64_t waves = tokens * g.slices * (kThreads / 64u) / per;   // of chunks of one position
-    uint32_t chunk = kMostPositions / kThreads;
+    uint32_t chunk = kShortestChunk;
     while (chunk < kMostChunk && per * chunk < kMostPositions &&
            (waves / (2u * chunk) >= 4096u || (waves / (2u * chunk) >= 1024u && tokens / chunk > 2048u))) {
         chunk *= 2u;
     }
     return chunk;
+}
+
+// Floats of one slot of all chunks' partial sums, for so many positions or fewer and rows of `width` values or less: longer chunks, of which
+// there are fewer, make the need itself fall where a batch grows.  chunk_of stops at one of three: chunks of kMostChunk; chunks of which a
+// workgroup's hold kMostPositions (2048 / chunk of them, each of 2048 values a workgroup's row at most: a float for every position); or fewer
+// than 4096 waves from chunks twice as long, which leaves at most 2048 * 2048 values.
+uint64_t most_partials(uint64_t tokens, uint64_t width) {
+    const uint64_t most = std::max<uint64_t>({2048u * 2048u, (tokens + kMostChunk - 1u) / kMostChunk * width, tokens}) + width;
+    return std::min((tokens + kShortestChunk - 1u) / kShortestChunk * width, most);
 }
 
 struct GradWorkspace {
@@ -916,9 +929,9 @@ struct GradWorkspace {
     float* partials;
     size_t bytes;
 };
+// Every part is the larger the more positions, values and rows there are, so that a workspace serves all smaller batches.
 GradWorkspace grad_workspace(void* base, uint64_t tokens, uint32_t dim, uint64_t rows) {
     GradWorkspace w = {};
-    if (few_positions(tokens, dim, rows)) return w;
     w.named = static_cast<uint32_t*>(base);
     w.bytes = (rows + 15u) & ~(uint64_t)15u;
     const SortShape s = sort_shape(tokens, rows);
@@ -932,11 +945,10 @@ GradWorkspace grad_workspace(void* base, uint64_t tokens, uint32_t dim, uint64_t
         w.keys[i] = take(tokens);
         w.order[i] = take(tokens);
     }
-    w.counts = take((uint64_t)s.ranges << s.bits);
-    const uint64_t chunks = (tokens + chunk_of(tokens, dim) - 1u) / chunk_of(tokens, dim);
+    w.counts = take(s.most_counts);
     w.join_counts = take(kJoinLists * kJoinLine);
-    w.joins = reinterpret_cast<uint2*>(take(2u * join_capacity(chunks)));
-    w.partials = reinterpret_cast<float*>(take(chunks * 2u * ((dim + 7u) & ~7u)));
+    w.joins = reinterpret_cast<uint2*>(take(2u * join_capacity((tokens + kShortestChunk - 1u) / kShortestChunk)));
+    w.partials = reinterpret_cast<float*>(take(2u * most_partials(tokens, (dim + 7u) & ~7u)));
     return w;
 }
 
@@ -955,7 +967,12 @@ hipError_t launch_embedding(const RowMatrix& table, const TokenIds& ids, uint32_
     return hipGetLastError();
 }
 
-size_t embedding_grad_workspace(uint64_t tokens, uint32_t dim, uint64_t rows) { return tokens == 0 ? 0 : grad_workspace(nullptr, tokens, dim, rows).bytes; }
+bool embedding_grad_takes_workspace(uint64_t tokens, uint32_t dim, uint64_t rows) { return tokens != 0 && !few_positions(tokens, dim, rows); }
+size_t embedding_grad_workspace(uint64_t tokens, uint32_t dim, uint64_t rows) {
+    // a table of fewer rows is sorted
+    if (!embedding_grad_takes_workspace(tokens, dim, rows)) rows = tokens == 0 ? 0 : (tokens - 1u) / kFewRun;
+    return rows == 0 ? 0 : grad_workspace(nullptr, tokens, dim, rows).bytes;
+}
 
 hipError_t launch_embedding_grad(const RowMatrix& grad_out, const TokenIds& ids, uint32_t dim, float scale, const RowMatrix& table_grad,
                                  bool accumulate, void* workspace, hipStream_t stream) {

@@ -273,7 +273,8 @@ struct TokenIds {
     int64_t first_row, padding;
 };
 hipError_t launch_embedding(const RowMatrix& table, const TokenIds& ids, uint32_t dim, float scale, const RowMatrix& out, hipStream_t stream);
-size_t embedding_grad_workspace(uint64_t tokens, uint32_t dim, uint64_t rows);
+size_t embedding_grad_workspace(uint64_t tokens, uint32_t dim, uint64_t rows);      // serves smaller batches too
+bool embedding_grad_takes_workspace(uint64_t tokens, uint32_t dim, uint64_t rows);   // whether a call of exactly these sizes uses it
 hipError_t launch_embedding_grad(const RowMatrix& grad_out, const TokenIds& ids, uint32_t dim, float scale, const RowMatrix& table_grad,
                                  bool accumulate, void* workspace, hipStream_t stream);
 

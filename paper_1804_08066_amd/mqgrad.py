@@ -979,7 +979,8 @@ def mqg_embedding_grad(grad_out, ids, rows, scale=1.0, first_row=0, padding_id=N
     """The gradient of mqg_embedding with respect to its table of `rows` rows: scale * the sum over the positions of every row's token of
     grad_out's rows, summed in fp32 and reproducible to the bit.  Positions of padding_id add to no row.  out: [rows, dim] of any of the
     three types, overwritten, or with accumulate=True added to (allocated here, in grad_out's type, when not given).  `workspace`: a
-    device tensor of at least mqg_embedding_grad_workspace_bytes(ids.numel(), dim, rows) bytes (allocated here when not given)."""
+    device tensor of at least mqg_embedding_grad_workspace_bytes(ids.numel(), dim, rows) bytes (allocated here when not given); one of
+    the size for the largest batch serves the smaller ones."""
     _lib or lib()
     if out is not None and workspace is not None:
         st = _marshal.embedding_grad(grad_out, ids, rows, scale, first_row, padding_id, out, accumulate, workspace, stream)
