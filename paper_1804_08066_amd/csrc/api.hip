@@ -161,13 +161,14 @@ struct Span {
     uint32_t item;
     bool written;
 };
-bool overlap(const Span& a, const Span& b) { return a.at < b.end && b.at < a.end; }
+// an empty one lies over nothing
+bool overlap(const Span& a, const Span& b) { return a.at < b.end && b.at < a.end && a.at < a.end && b.at < b.end; }
 Span span_of(const void* p, uint64_t bytes, uint32_t item = 0u, bool written = false) {
     const uintptr_t at = reinterpret_cast<uintptr_t>(p);
     return {at, at + bytes, item, written};
 }
 
-// Whether a written span of `spans` lies over any other, an item's own two being the same span excepted.  Sorts them.
+// Whether a written span of `spans`, none of which is empty, lies over any other, an item's own two being the same span excepted.  Sorts them.
 bool writes_collide(Span* spans, uint32_t count) {
     std::sort(spans, spans + count, [](const Span& a, const Span& b) { return a.at < b.at; });
     // the span seen so far that ends last, and the last such of another item; of the written ones, and of all
@@ -233,7 +234,7 @@ mqg_status clip_items(const mqg_clip_item* items, uint32_t count, double max_nor
         spans[used++] = out;
     }
     spans[used++] = span_of(norm, sizeof(double), count + 1u, scratch != nullptr);
-    if (scratch != nullptr) spans[used++] = span_of(scratch, scratch_bytes, count + 2u, true);
+    if (scratch_bytes != 0) spans[used++] = span_of(scratch, scratch_bytes, count + 2u, true);
     bad = bad || writes_collide(spans, used);
     if (spans != few) delete[] spans;
     return bad ? MQG_EINVAL : MQG_OK;

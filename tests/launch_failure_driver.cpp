@@ -1,10 +1,11 @@
 // Drives the norm, clipping and embedding entry points over a stand-in for the runtime's launch: nothing runs, launches are counted, and one of
-// them can be made to fail.  The error of a launch is held until the next launch only, which is all that the library may rely on.  Prints what
-// went wrong, or "ok".  Host only: the addresses are invented, and no launch reaches a GPU.
+// them can be made to fail.  The error of a launch is held until the next launch only, which is all that the library may rely on.  The argument
+// names the checks: failures, empty.  Prints what went wrong, or "ok".  Host only: the addresses are invented, and no launch reaches a GPU.
 #include <hip/hip_runtime_api.h>
 
 #include <cstdint>
 #include <cstdio>
+#include <cstring>
 #include <functional>
 #include <vector>
 
@@ -60,7 +61,7 @@ static mqg_status gradient(uint64_t tokens, uint32_t dim, uint64_t rows, int acc
     return mqg_embedding_grad(&g, &ids, dim, 1.0f, &out, accumulate, at(192), nullptr);
 }
 
-int main() {
+static void failures() {
     for (int accumulate = 0; accumulate < 2; ++accumulate) {
         check("gradient, no positions", 1 - accumulate, [&] { return gradient(0, 64, 1000, accumulate); });
         check("gradient, direct", 1, [&] { return gradient(100, 64, 1000, accumulate); });
@@ -85,6 +86,35 @@ int main() {
             check("norm and clip", norms + finish + clips, [&] { return mqg_clip_global_norm(items.data(), count, 1.0, at(1001), norm, nullptr); });
         }
     }
+}
+
+// tensors, rows and tokens of which there are none lie over nothing, wherever their addresses point
+static void empty() {
+    char *scratch = static_cast<char*>(at(10)), *norm = static_cast<char*>(at(11)), *values = static_cast<char*>(at(12)), *out = static_cast<char*>(at(13));
+    for (char* inside : {scratch + 64, norm + 4, values + 8, out + 8}) {
+        std::vector<mqg_clip_item> items = {{values, out, 1000, MQG_FLOAT32, MQG_FLOAT32}, {inside, inside, 0, MQG_FLOAT32, MQG_BFLOAT16}};
+        check("norm with an empty tensor", 2, [&] { return mqg_global_norm(items.data(), 2, scratch, (double*)norm, nullptr); });
+        check("clip by a norm with an empty tensor", 1, [&] { return mqg_clip_by_norm(items.data(), 2, (double*)norm, 1.0, nullptr); });
+        check("norm and clip with an empty tensor", 2, [&] { return mqg_clip_global_norm(items.data(), 2, 1.0, scratch, (double*)norm, nullptr); });
+    }
+    check("norm and clip of nothing", 1, [&] { return mqg_clip_global_norm(nullptr, 0, 1.0, norm, (double*)norm, nullptr); });
+    check("norm of nothing", 1, [&] { return mqg_global_norm(nullptr, 0, norm, (double*)norm, nullptr); });
+    const mqg_rows table = {values, 1000, 64, MQG_FLOAT32};
+    for (char* inside : {values + 64, values}) {
+        const mqg_rows none = {inside, 0, 64, MQG_FLOAT32};
+        const mqg_tokens ids = {inside, 0, MQG_INDEX32, 0, INT64_MIN};
+        check("lookup of no tokens", 0, [&] { return mqg_embedding(&table, &ids, 64, 1.0f, &none, nullptr); });
+        check("gradient of no positions", 1, [&] { return mqg_embedding_grad(&none, &ids, 64, 1.0f, &table, 0, inside, nullptr); });
+        const mqg_rows few = {out, 10, 64, MQG_FLOAT32};   // whose sums take no workspace
+        const mqg_tokens tokens = {scratch, 10, MQG_INDEX32, 0, INT64_MIN};
+        check("gradient without scratch memory", 1, [&] { return mqg_embedding_grad(&few, &tokens, 64, 1.0f, &table, 0, inside, nullptr); });
+    }
+}
+
+int main(int argc, char** argv) {
+    if (argc == 2 && std::strcmp(argv[1], "failures") == 0) failures();
+    else if (argc == 2 && std::strcmp(argv[1], "empty") == 0) empty();
+    else return 2;
     if (g_wrong == 0) std::printf("ok\n");
     return g_wrong == 0 ? 0 : 1;
 }
