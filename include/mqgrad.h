@@ -403,7 +403,7 @@ mqg_status mqg_adaptive_bits(const double* worker_norms, uint32_t W, const mqg_a
  *
  *   norm = sqrt(sum over all tensors and values of x^2)     squares and sums in fp64
  *   c    = 1 where norm <= max_norm, else (float)(max_norm / norm);  a norm that is not a number makes c one too
- *   y    = x * c, one fp32 product, rounded once to the output's type
+ *   y    = x * c, one fp32 product; a half-precision y is the value nearest to it (either of two)
  *
  * Where a gradient is quantized already, its scales (or ranges) are clipped in its stead: a bucket's levels are
  * proportional to its scale, so mqg_global_norm of the gradients and mqg_clip_by_norm of the scales give the clipped
@@ -421,8 +421,8 @@ typedef struct {
     mqg_dtype out_dtype;  /* not read by mqg_global_norm */
 } mqg_clip_item;
 
-/* The norm of all `count` tensors together; reproducible to the bit (the order of all additions depends on the sizes
- * only).  A tensor named twice counts twice.
+/* The norm of all `count` tensors together; reproducible to the bit (the order of all additions depends on the
+ * tensors' order, sizes and types only).  A tensor named twice counts twice.
  *   items       HOST array of `count` tensors, at most MQG_MAX_NORM_TENSORS, read during the call only.
  *   workspace   device, mqg_global_norm_workspace_bytes(count) bytes of scratch memory, 8-byte aligned; contents on
  *               entry are of no interest, contents on return are unspecified.  Calls that share a workspace must not overlap.
@@ -452,14 +452,16 @@ mqg_status mqg_clip_global_norm(const mqg_clip_item* items, uint32_t count, doub
  * server's (or a shard's) rows are looked up by token, and the gradient of the rows is added up by token, either as a
  * whole table (which is clipped, quantized and exchanged like any other layer) or straight into the parameters:
  *
- *   lookup    out[p, :]   = scale * table[id_p - first_row, :]          (fp32 product, rounded once to out's type)
+ *   lookup    out[p, :]   = scale * table[id_p - first_row, :]          (one fp32 product; a half-precision value is the nearest to it)
  *   gradient  grad[r, :]  = scale * S_r,                                S_r = sum over the positions p with
  *             grad[r, :] += scale * S_r  (accumulate)                   id_p - first_row = r of grad_out[p, :]
  *
  * A token outside [first_row, first_row + rows) belongs to another shard (or is a filler such as -1): its row of `out` is
- * zero and its position adds to no row.  S_r is summed in fp32 in an order that depends on the tokens only (equal inputs
- * give equal bits) and rounded once, after the product with scale and the addition to the old value.  Every row that no
- * token names becomes zero; with `accumulate` it is left untouched.  With scale = -lr (or -lr / W for the positions of W
+ * zero and its position adds to no row.  S_r is summed in fp32 in an order that depends on the tokens, first_row, padding_id,
+ * dim, rows and accumulate only: equal calls give equal bits, while a shard's rows, or a slice of the columns, agree with
+ * the whole table's within the sums' roundings.  The product with scale, or the multiply-add to the old value, is rounded
+ * to fp32; a half-precision output is the value nearest to that (either of two).  Every row that no token names becomes zero; with
+ * `accumulate` it is left untouched.  With scale = -lr (or -lr / W for the positions of W
  * workers, one after the other), accumulate and the parameters in the place of grad, that is the server's SGD step from
  * gradients that are sparse by rows. */
 
@@ -486,7 +488,8 @@ typedef struct {
 
 /* table: `rows` rows, read; out: tokens->count rows, overwritten (data may be NULL where there are none).  1 <= dim <= MQG_MAX_ROW_DIM.
  * Errors: MQG_EINVAL (NULL pointer, size or type out of range, rows of `out` that overlap each other, out->rows other than
- * tokens->count, `out` over the table or the tokens), MQG_EALIGN, MQG_ELAUNCH. */
+ * tokens->count, `out` over the table or the tokens), MQG_EALIGN, MQG_ELAUNCH.  A matrix lies over all memory from its first
+ * value to its last: other columns of the same buffer are refused too. */
 mqg_status mqg_embedding(const mqg_rows* table, const mqg_tokens* tokens, uint32_t dim, float scale, const mqg_rows* out, void* stream);
 
 /* grad_out: tokens->count rows, read; table_grad: `rows` rows, overwritten or added to.
@@ -494,7 +497,7 @@ mqg_status mqg_embedding(const mqg_rows* table, const mqg_tokens* tokens, uint32
  *               aligned; contents on entry are of no interest, contents on return are unspecified.  Calls that share a
  *               workspace must not overlap.  May be NULL where that size is 0.  The size for the largest of several batches
  *               is enough for each: it does not fall as any of the three grows.
- * Errors as for mqg_embedding. */
+ * Errors as for mqg_embedding; MQG_EINVAL also where table_grad or the workspace lies over grad_out, the tokens or each other. */
 size_t mqg_embedding_grad_workspace_bytes(uint64_t tokens, uint32_t dim, uint64_t rows);
 mqg_status mqg_embedding_grad(const mqg_rows* grad_out, const mqg_tokens* tokens, uint32_t dim, float scale, const mqg_rows* table_grad,
                               int accumulate, void* workspace, void* stream);
