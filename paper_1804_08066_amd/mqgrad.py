@@ -949,7 +949,8 @@ _NO_PADDING = -(1 << 63)
 
 def mqg_embedding(table, ids, scale=1.0, first_row=0, out=None, stream=None):
     """scale * table[ids - first_row], rows of zeros for tokens outside the table.  table: [rows, dim], rows at any stride; ids: int32 or
-    int64, of any shape; out: [*ids.shape, dim] of any of the three types (allocated here, in the table's type, when not given)."""
+    int64, of any shape; out: [*ids.shape, dim] of any of the three types (allocated here, in the table's type, when not given).  Autograd
+    does not see the call, a table that requires a gradient included: mqg_embedding_grad of the rows' gradient is that gradient."""
     _lib or lib()
     if out is not None:
         st = _marshal.embedding(table, ids, scale, first_row, out, stream)
@@ -977,7 +978,7 @@ def mqg_embedding_grad_workspace_bytes(tokens, dim, rows):
 
 def mqg_embedding_grad(grad_out, ids, rows, scale=1.0, first_row=0, padding_id=None, out=None, accumulate=False, workspace=None, stream=None):
     """The gradient of mqg_embedding with respect to its table of `rows` rows: scale * the sum over the positions of every row's token of
-    grad_out's rows, summed in fp32 and reproducible to the bit.  Positions of padding_id add to no row.  out: [rows, dim] of any of the
+    grad_out's rows, summed in fp32 (equal calls give equal bits).  Positions of padding_id add to no row.  out: [rows, dim] of any of the
     three types, overwritten, or with accumulate=True added to (allocated here, in grad_out's type, when not given).  `workspace`: a
     device tensor of at least mqg_embedding_grad_workspace_bytes(ids.numel(), dim, rows) bytes (allocated here when not given); one of
     the size for the largest batch serves the smaller ones."""
