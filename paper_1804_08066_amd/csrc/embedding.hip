@@ -510,12 +510,18 @@ __global__ __launch_bounds__(kOneThreads) void sort_buckets_kernel(const SortArg
 // ---- a few positions ------------------------------------------------------------------------------------
 // Without a sort: every workgroup finds the positions of its position's row among all of them, a quarter a wave, and adds up their
 // slice of grad_out where its own is the first.  One launch, whose work is the square of the positions for every slice of 256 values.
-// kFewWork: below it this is faster than sort, sums and joins (half-precision rows into fp32, positions x values, this and those:
-// 1000 x 1000 8.9 and 17.7 us; 2000 x 64 8.8 and 19.7; 2000 x 500 11.9 and 19; 3300 x 250 16.4 and 20.6; 4000 x 250 19 and 20.6;
-// 2000 x 1000 21 and 19.7; 2600 x 500 21 and 19.8).
+// kFewWork: this is faster than sort, sums and joins, or level, for rows of several slices up to half of it and for rows of one slice up to
+// all of it, but for 250 values and rows to clear; above half, rows of several slices take up to 45 % longer.  (Half-precision rows added to
+// fp32 ones, positions x values, this and those: 500 x 512 4.2 and 14.6 us; 1000 x 1000 8.6 and 16.0; 2000 x 64 8.4 and 18.7; 2000 x 500 11.4
+// and 17.6; 3300 x 250 16.1 and 19.2; 4000 x 16 18.3 and 23.2; 4000 x 250 18.8 and 19.5; 1700 x 1000 17.0 and 17.8; 2600 x 500 20.8 and 18.4;
+// 2000 x 1000 20.4 and 18.7; 1200 x 2500 26.5 and 18.3.  With 20000 fp32 rows cleared beside: 1000 x 1000 23.0 and 25.2; 2000 x 500 17.9 and 20.4;
+// 4000 x 250 22.7 and 19.7; 2000 x 1000 32.4 and 27.1.)  The slices are counted as fp32 values have them; half precision on both sides has half
+// as many (with 20000 rows cleared, 2000 x 1000 17.8 and 21.3; 2600 x 500 15.7 and 19.8).
 constexpr uint32_t kFewTokens = 4096, kFewSum = 8, kFewRows = 1024;
 constexpr uint64_t kFewWork = 16000000;
-// Few rows of the table have long runs, which one workgroup adds up (2000 positions of 64 values in 4 rows: 29 us against 16).
+// Few rows of the table have long runs, which one workgroup adds up (2000 positions of 64 values in 4 rows: 29 us against 16).  In a larger
+// table a row that most positions name is not foreseen (4000 positions of 250 values, all of one row: 128 us against 31, half of them 60
+// against 25; 1000 positions 30 and 17.6 against 20 and 19).
 constexpr uint32_t kFewRun = 256;   // positions of a row, on average
 bool few_positions(uint64_t tokens, uint32_t dim, uint64_t rows) {
     return tokens <= kFewTokens && tokens <= kFewRun * rows && tokens * tokens * ((dim + 255u) / 256u) <= kFewWork;
@@ -532,7 +538,7 @@ struct FewArgs {
 __device__ __forceinline__ uint32_t few_row(const TokenIds& t, uint32_t i, uint32_t rows) {
     return t.wide ? row_of<true>(t, i, rows, true) : row_of<false>(t, i, rows, true);
 }
-// ITEMS: positions that a lane searches at most (1000 positions of 1000 values, 8 and 4: 10.7 and 8.9 us)
+// ITEMS: positions that a lane searches at most (1000 positions of 1000 values, 8 and 4: 10.7 and 8.9 us; 512 of 4096, 4 and 2: 12.9 and 11.3)
 template <int IN, int OUT, uint32_t ITEMS>
 __global__ __launch_bounds__(kThreads) void sum_few_kernel(const FewArgs a) {
     constexpr int V = values_of(IN, OUT);
